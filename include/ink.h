@@ -36,7 +36,7 @@
  *     Edge (u -> v) makes u an in-neighbour of v: v aggregates m_u.
  *   - At most 2^31 - 2^30 - 1 edges (event offsets are 32-bit); a batch that could take the graph
  *     past that is refused.
- *   - All matrices are row-major float32.  Layer outputs are at most INK_MAX_OUT_DIM wide, layer
+ *   - All matrices of a context are row-major float32.  Layer outputs are at most INK_MAX_OUT_DIM wide, layer
  *     inputs (the feature width in particular) at most INK_MAX_IN_DIM.
  */
 #ifndef INK_H
@@ -52,6 +52,8 @@ extern "C" {
 #define INK_MAX_OUT_DIM 256
 #define INK_MAX_IN_DIM 16384
 #define INK_MAX_LAYERS 8
+#define INK_MAX_CLASSES (1 << 30) /* ink_log_probs: classes of a row, and alternatives asked for */
+#define INK_MAX_TOP 16
 
 typedef struct ink_ctx ink_ctx; /* opaque; owns all device state */
 
@@ -75,7 +77,10 @@ typedef enum {
   INK_AGG_MAX = 0, INK_AGG_MIN = 1, INK_AGG_SUM = 2, INK_AGG_MEAN = 3, INK_AGG_GCN_SYM = 4
 } ink_agg;
 
-typedef enum { INK_ACT_NONE = 0, INK_ACT_RELU = 1 } ink_act;
+/* GELU (z times the normal distribution function) and SILU (z times the logistic function): ink_linear only,
+ * a layer takes NONE or RELU. */
+typedef enum { INK_ACT_NONE = 0, INK_ACT_RELU = 1, INK_ACT_GELU = 2, INK_ACT_SILU = 3 } ink_act;
+typedef enum { INK_F32 = 0, INK_BF16 = 1, INK_F16 = 2 } ink_type; /* element types of an answer head's operators */
 typedef enum { INK_MEM_HOST = 0, INK_MEM_DEVICE = 1 } ink_mem;
 
 /* In-neighbour CSR of the initial snapshot: row v lists the sources u of edges u -> v,
@@ -341,8 +346,86 @@ ink_status ink_set_profiling(ink_ctx *ctx, int32_t on);
 /* Copies min(bytes, sizeof(ink_stats)) bytes of the last call's statistics. */
 ink_status ink_get_stats(ink_ctx *ctx, void *stats_out, size_t bytes);
 
+/* ---------------------------------------------------------------- operators of an answer head
+ *
+ * What turns embeddings into answers, and re-fits that map while the graph changes: layer norm, a
+ * linear layer with its epilogue, log probabilities of classes; each with its gradient.  They need no context
+ * and take rows from anywhere on the device, an update's result (ink_update_result) among them.
+ *
+ * Unlike the calls on a context these are ASYNCHRONOUS: a call enqueues its kernels on `hip_stream`
+ * (NULL: the default stream) of the current device and returns; it allocates nothing, keeps nothing and never waits, so
+ * it can be captured into a graph.  Every pointer is DEVICE memory that has to stay valid, unchanged
+ * and ready on that stream until the work is done; outputs must overlap neither inputs nor each other.  Where a call
+ * needs `work` memory, its ..._work function says how many bytes (0: none, NULL will do); a
+ * work buffer serves one call at a time.  The same call on the same inputs gives the same bits.
+ *
+ * Matrices are row-major, of ink_type elements, row i at i * ld elements.  ld is any number from the
+ * row's length up; a matrix that is read may also have ld = 0, one row for all.  Pointers need the alignment of an
+ * element only.  No rows are allowed (outputs of whole-batch sums are then zeros).  Sums and statistics are kept in 32 bits,
+ * outputs are rounded once, to nearest even.  NaN and infinities go where the formulas take them.
+ *
+ * Errors: INK_E_ARG (NULL, misaligned or too little memory, sizes or types out of range, an unknown activation), INK_E_RANGE,
+ * INK_E_DEVICE (a launch was refused); ink_last_error(NULL) has the message.  After an argument error nothing was enqueued. */
+
+/* y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(var + eps), mean and (biased) variance of each row.
+ *   x, y         [rows][cols] of `type`, cols 1 .. INK_MAX_IN_DIM
+ *   weight, bias [cols] of `param_type` (`type` or INK_F32), or NULL: 1 and 0
+ *   mean, rstd   [rows] float, written for the gradient, or NULL
+ *   eps          > 0 */
+ink_status ink_layer_norm(const void *x, int64_t ld_x, const void *weight, const void *bias, int64_t rows, int32_t cols,
+                          int32_t type, int32_t param_type, float eps, void *y, int64_t ld_y, float *mean, float *rstd,
+                          void *hip_stream);
+
+/* Gradient of ink_layer_norm: dx [rows][cols] of `type`, dweight and dbias [cols] of `param_type`, summed over the rows; each
+ * may be NULL (not wanted).  mean and rstd as the forward call wrote them. */
+size_t ink_layer_norm_backward_work(int64_t rows, int32_t cols, int32_t type);
+ink_status ink_layer_norm_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const float *mean,
+                                   const float *rstd, const void *weight, int64_t rows, int32_t cols, int32_t type,
+                                   int32_t param_type, void *dx, int64_t ld_dx, void *dweight, void *dbias, void *work,
+                                   size_t work_bytes, void *hip_stream);
+
+/* y = act(z) + residual, z = x W + bias.
+ *   x            [rows][cols] of `type`; W [cols][out] and bias [out] (or NULL) of `type`; cols and out 1 .. INK_MAX_IN_DIM
+ *   residual     [rows][out] of `out_type`, or NULL
+ *   y, pre       [rows][out] of `out_type` (`type` or INK_F32: logits of 16-bit rows); pre, where not NULL, gets z for the gradient
+ *   act          ink_act */
+ink_status ink_linear(const void *x, int64_t ld_x, const void *weight, int64_t ld_w, const void *bias, const void *residual,
+                      int64_t ld_res, int64_t rows, int32_t cols, int32_t out, int32_t type, int32_t out_type, int32_t act,
+                      void *y, int64_t ld_y, void *pre, int64_t ld_pre, void *hip_stream);
+
+/* Gradient of ink_linear (that of the residual is dy itself): dz = dy * act'(pre), dx = dz W^T [rows][cols], dweight = x^T dz
+ * [cols][out], dbias [out] = sum of dz over the rows, all of `type`; each may be NULL (not wanted).
+ *   dy, pre      [rows][out] of `dy_type` (`type`, or INK_F32 with INK_BF16); pre is not read for INK_ACT_NONE
+ * With 16-bit rows dz is rounded to `type` before the two products. */
+size_t ink_linear_backward_work(int64_t rows, int32_t cols, int32_t out);
+ink_status ink_linear_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const void *weight, int64_t ld_w,
+                               const void *pre, int64_t ld_pre, int64_t rows, int32_t cols, int32_t out, int32_t type,
+                               int32_t dy_type, int32_t act, void *dx, int64_t ld_dx, void *dweight, int64_t ld_dw, void *dbias,
+                               void *work, size_t work_bytes, void *hip_stream);
+
+/* For each row of logits, with z = scale * logit and p = softmax(z):
+ *   logp      [rows] log p of the row's target; 0 for a row without one (a target outside [0, classes), or targets NULL)
+ *   entropy   [rows] -sum p log p
+ *   lse       [rows] log sum exp z
+ *   top_ids   [rows][top] the classes of the `top` largest logits, largest first; equal logits by the lower class, NaN
+ *             first of all; top_logp [rows][top] their log p.  top 0 .. min(classes, INK_MAX_TOP)
+ * Each output may be NULL.  targets: int32 (target_bytes 4) or int64 (8).  A class at -inf is masked.  In a row of masked
+ * classes lse and every log p is -inf and the entropy 0; a NaN or +inf among the logits makes lse, entropy and log p NaN.
+ *   scale     > 0 (1 / temperature);  classes 1 .. INK_MAX_CLASSES */
+size_t ink_log_probs_work(int64_t rows, int64_t classes, int32_t type, int32_t top);
+ink_status ink_log_probs(const void *logits, int64_t ld, const void *targets, int32_t target_bytes, int64_t rows, int64_t classes,
+                         int32_t type, float scale, int32_t top, float *logp, float *entropy, float *lse, int32_t *top_ids,
+                         float *top_logp, void *work, size_t work_bytes, void *hip_stream);
+
+/* Gradient of sum_r g_logp[r] logp[r] + g_entropy[r] entropy[r] by the logits, [rows][classes] of `type` (not that of lse or
+ * top_logp).  Either of g_logp and g_entropy may be NULL; lse and entropy as the forward call wrote them (entropy
+ * is read with g_entropy only).  A row without a target takes no part in g_logp; a row of masked classes has gradient 0. */
+ink_status ink_log_probs_backward(const void *logits, int64_t ld, const void *targets, int32_t target_bytes, const float *lse,
+                                  const float *entropy, const float *g_logp, const float *g_entropy, int64_t rows, int64_t classes,
+                                  int32_t type, float scale, void *dlogits, int64_t ld_out, void *hip_stream);
+
 /* Message of the last failing call on this context ("" if none).  ctx may be NULL: then the
- * message of the last failing ink_create on this thread. */
+ * message of the last failing ink_create or operator of an answer head on this thread. */
 const char *ink_last_error(const ink_ctx *ctx);
 
 void ink_destroy(ink_ctx *ctx);

@@ -4,6 +4,7 @@
 // on the changed rows -> compare-and-emit the next layer's sources.
 #include <algorithm>
 #include <chrono>
+#include <cstdarg>
 #include <cstring>
 #include <cstdio>
 #include <mutex>
@@ -12,6 +13,7 @@
 
 #include "bigrows.h"
 #include "events.h"
+#include "head.h"
 
 using namespace ink;
 
@@ -639,6 +641,19 @@ static ink_status fail(ink_ctx *c, ink_status st, const std::string &msg) {
   if (c) c->err = msg; else g_create_err = msg;
   return st;
 }
+
+// The operators of an answer head have no context: their message is this thread's, like ink_create's.
+namespace ink {
+ink_status fail_call(ink_status st, const char *fmt, ...) noexcept {
+  char msg[256];
+  va_list args;
+  va_start(args, fmt);
+  vsnprintf(msg, sizeof msg, fmt, args);
+  va_end(args);
+  try { g_create_err = msg; } catch (...) {}       // no memory for the message: the status says enough
+  return st;
+}
+}  // namespace ink
 
 // What a failing call had enqueued by then may read the caller's arrays: it has ended before the call returns.
 static ink_status drain(ink_ctx *c, ink_status st) {
