@@ -15,12 +15,14 @@
 // sums the unrounded values.  dweight is a sum over all rows: workgroups take slices of the rows and leave a
 // partial matrix each, which k_weight_sum adds up in order (no atomics: the same call gives the same bits).
 #include <algorithm>
+#include <type_traits>
 
 #include "head.h"
 
 namespace ink {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float F4 __attribute__((ext_vector_type(4)));
 
 template <class T> struct Frag;              // 16 bytes of a row or of a column: what one lane gives a matrix instruction
 template <> struct Frag<float> { typedef float V __attribute__((ext_vector_type(4))); };
@@ -35,6 +37,22 @@ __device__ __forceinline__ f32x16 mma(Frag<float>::V a, Frag<float>::V b, f32x16
 #pragma unroll
   for (int j = 0; j < 4; j++) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
   return c;
+}
+// Several products of one step: in 32 bits a step is four instructions, and those of one accumulator do not follow each other.
+template <class T, int M, int N> __device__ __forceinline__ void mma_block(const typename Frag<T>::V (&a)[N], const typename Frag<T>::V (&b)[M], f32x16 (&c)[M][N]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+#pragma unroll
+      for (int i = 0; i < M; i++)
+#pragma unroll
+        for (int n = 0; n < N; n++) c[i][n] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[n][j], b[i][j], c[i][n], 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < M; i++)
+#pragma unroll
+      for (int n = 0; n < N; n++) c[i][n] = mma(a[n], b[i], c[i][n]);
+  }
 }
 // Where a product's element stands in a lane: column (of the second operand) lane % 32, row 8 (e / 4) + 4 (lane / 32) + e % 4.
 
@@ -61,6 +79,31 @@ __device__ __forceinline__ float activate_grad(float z, int act) {
   if (act == INK_ACT_GELU) { float pdf; const float cdf = normal_cdf(z, pdf); return fmaf(z, pdf, cdf); }
   if (act == INK_ACT_SILU) { const float s = sigmoid(z); return s * fmaf(z, 1.f - s, 1.f); }
   return 1.f;
+}
+
+// the same of several elements, one decision for all of them
+template <int N> __device__ __forceinline__ void activate_all(float v[N], int act) {
+  if (act == INK_ACT_NONE) return;
+  if (act == INK_ACT_RELU)
+#pragma unroll
+    for (int e = 0; e < N; e++) v[e] = activate(v[e], INK_ACT_RELU);
+  else if (act == INK_ACT_GELU)
+#pragma unroll
+    for (int e = 0; e < N; e++) v[e] = activate(v[e], INK_ACT_GELU);
+  else
+#pragma unroll
+    for (int e = 0; e < N; e++) v[e] = activate(v[e], INK_ACT_SILU);
+}
+template <int N> __device__ __forceinline__ void scale_by_slope(float d[N], const float z[N], int act) {
+  if (act == INK_ACT_RELU)
+#pragma unroll
+    for (int e = 0; e < N; e++) d[e] *= activate_grad(z[e], INK_ACT_RELU);
+  else if (act == INK_ACT_GELU)
+#pragma unroll
+    for (int e = 0; e < N; e++) d[e] *= activate_grad(z[e], INK_ACT_GELU);
+  else
+#pragma unroll
+    for (int e = 0; e < N; e++) d[e] *= activate_grad(z[e], INK_ACT_SILU);
 }
 
 struct LinearArgs {
@@ -152,76 +195,402 @@ template <class T> __device__ __forceinline__ void store4(T *p, int c, int n, co
 
 constexpr int kLinearThreads = 512;
 
+// Four neighbouring columns of a row of results, from the registers of the products: bias, z, activation, residual, y.
+template <class T, class TO, bool GRAD> __device__ __forceinline__ void finish4(const LinearArgs &a, int64_t r, int c, float v[4]) {
+  if constexpr (!GRAD) {
+    float q[4];
+    if (a.bias) {
+      load4(static_cast<const T *>(a.bias), c, a.width, q);
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[j] += q[j];
+    }
+    if (a.keep) store4(static_cast<TO *>(a.keep) + r * a.ld_keep, c, a.width, v);
+    activate_all<4>(v, a.act);
+    if (a.res) {
+      load4(static_cast<const TO *>(a.res) + r * a.ld_res, c, a.width, q);
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[j] += q[j];
+    }
+  }
+  store4(static_cast<TO *>(a.out) + r * a.ld_out, c, a.width, v);
+}
+
+// a fragment of a row of rows read: x, or dz of dy and z
+template <class T, class TI, bool GRAD> __device__ __forceinline__ typename Frag<T>::V in_frag(const LinearArgs &a, int64_t r, int k) {
+  const TI *x = static_cast<const TI *>(a.in) + r * a.ld_in;
+  if constexpr (GRAD) return grad_frag<T, TI>(x, static_cast<const TI *>(a.pre) + (a.pre ? r * a.ld_pre : 0), k, a.depth, a.act);
+  else return row_frag<T>(x, k, a.depth);
+}
+
+// ------------------------------------------------------------------------------------ tiles
 // T: type of the operands, TI: of the rows read (GRAD: dy and z), TO: of the rows written.
-template <class T, class TI, class TO, int NT, bool GRAD>
-__global__ __launch_bounds__(kLinearThreads) void k_linear(LinearArgs a) {
+// 128 rows by 64 NTW columns a workgroup, 64 by 32 NTW a wave, 128 bytes of the depth in LDS at a time: while one piece is
+// multiplied the next is on its way in registers.  For 32-bit rows, which the matrix unit bounds, and depths whose W the registers of a
+// workgroup do not hold.  One buffer and three workgroups a CU against two buffers (one barrier a piece) and two workgroups: 233k x 602 x 256
+// f32 782 and 815 us; tiles of 64 rows and four workgroups 789.
+template <class T, class TI, class TO, int NTW, bool GRAD>
+__global__ __launch_bounds__(256, 3) void k_linear_tile(LinearArgs a) {
   typedef typename Frag<T>::V V;
-  constexpr int VK = kVec<T>, KS = kStep<T>, U = 4;
-  extern __shared__ __align__(16) char s_mem[];
-  V *s_w = reinterpret_cast<V *>(s_mem);
-  const int l = lane_id(), half = l / 32, waves = blockDim.x / kWave;
-  const int n0 = blockIdx.y * (NT * 32);
-  const bool resident = a.chunk >= a.depth;
-  const int64_t tile = 32 * (int64_t)waves, tiles = (a.rows + tile - 1) / tile;
-  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int64_t mine = t * tile + (threadIdx.x / kWave) * 32 + l % 32;
-    const int64_t r = mine < a.rows ? mine : a.rows - 1;
-    const TI *in = static_cast<const TI *>(a.in) + r * a.ld_in;
-    const TI *pre = static_cast<const TI *>(a.pre) + (a.pre ? r * a.ld_pre : 0);
-    f32x16 acc[NT];
+  constexpr int VK = kVec<T>, KC = 8 * VK, BM = 128, BN = 64 * NTW, NT = 2 * NTW, P = 9;      // P: 16-byte pieces between rows of x
+  constexpr int NX = BM * 8 / 256;
+  constexpr int NW = GRAD ? BN * 8 / 256 : VK, SQ = BN / VK * 8;           // W in pieces of its rows, or in squares (forward)
+  __shared__ V s_x[BM * P], s_w[BN * 8];
+  const int tid = threadIdx.x, l = lane_id(), half = l / 32, wm = tid / kWave / 2, wn = tid / kWave % 2;
+  // workgroups go to the eight chiplets in turn: the column tiles of the same rows are eight apart, so that one L2 serves them
+  const int gy = (a.width + BN - 1) / BN, id = blockIdx.x / 8;
+  const int64_t m0 = ((int64_t)(id / gy) * 8 + blockIdx.x % 8) * BM;
+  const int n0 = id % gy * BN;
+  if (m0 >= a.rows) return;
+  const T *w = static_cast<const T *>(a.weight);
+  V x[NX], wv[NW];
+  const int kp = tid % 8 * VK;               // this thread's place in 128 bytes of the depth
+  const TI *xp[NX], *zp[NX];
 #pragma unroll
-    for (int i = 0; i < NT; i++) acc[i] = f32x16{};
-    for (int k0 = 0; k0 < a.depth; k0 += a.chunk) {
-      const int len = min(a.chunk, (a.depth - k0 + KS - 1) / KS * KS);
-      if (!resident || t == blockIdx.x) {
-        __syncthreads();
-        stage_weights<T, NT, GRAD>(a, s_w, k0, len, n0);
-        __syncthreads();
-      }
-      for (int s0 = 0; s0 < len / KS; s0 += U) {
-        V x[U];
+  for (int j = 0; j < NX; j++) {
+    const int64_t r = min(m0 + tid / 8 + 32 * j, a.rows - 1);
+    xp[j] = static_cast<const TI *>(a.in) + r * a.ld_in;
+    zp[j] = GRAD && a.pre ? static_cast<const TI *>(a.pre) + r * a.ld_pre : nullptr;
+  }
+  const int wn_at = GRAD ? tid / 8 : tid % (BN / VK) * VK, wk_at = GRAD ? kp : tid / (BN / VK) * VK;      // first column, first k
+  const bool inside = n0 + BN <= a.width;
+  auto fetch = [&](int k0) {
+    const bool whole = k0 + KC <= a.depth;   // no piece is cut by the end of the depth
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-          const int k = k0 + (s0 + u) * KS + half * VK;
-          if constexpr (GRAD) x[u] = grad_frag<T, TI>(in, pre, k, a.depth, a.act);
-          else x[u] = row_frag<T>(in, k, a.depth);
+    for (int j = 0; j < NX; j++) {
+      if constexpr (GRAD) x[j] = grad_frag<T, TI>(xp[j], zp[j], k0 + kp, whole ? 0x7fffffff : a.depth, a.act);
+      else x[j] = row_frag<T>(xp[j], k0 + kp, whole ? 0x7fffffff : a.depth);
+    }
+    if (whole && inside) {
+      if (GRAD || tid < SQ)
+#pragma unroll
+        for (int j = 0; j < NW; j++) {
+          const T *at = w + (GRAD ? (int64_t)(n0 + wn_at + 32 * j) * a.ld_w + k0 + wk_at : (int64_t)(k0 + wk_at + j) * a.ld_w + n0 + wn_at);
+          wv[j] = (V)*reinterpret_cast<const typename Pack<T, VK>::type *>(at);
         }
+      return;
+    }
 #pragma unroll
-        for (int u = 0; u < U; u++)
-          if (s0 + u < len / KS)
+    for (int j = 0; j < NW; j++) {
+      wv[j] = V{};
+      const int n = n0 + wn_at + (GRAD ? 32 * j : 0), k = k0 + wk_at + (GRAD ? 0 : j);
+      if ((!GRAD && tid >= SQ) || k >= a.depth || n >= a.width) continue;
+      if constexpr (GRAD) wv[j] = row_frag<T>(w + (int64_t)n * a.ld_w, k, a.depth);
+      else wv[j] = row_frag<T>(w + (int64_t)k * a.ld_w, n, a.width);
+    }
+  };
+  auto put = [&]() {
 #pragma unroll
-            for (int i = 0; i < NT; i++) acc[i] = mma(s_w[((s0 + u) * NT + i) * 64 + l], x[u], acc[i]);
+    for (int j = 0; j < NX; j++) s_x[(tid / 8 + 32 * j) * P + tid % 8] = x[j];
+    if constexpr (GRAD) {
+#pragma unroll
+      for (int j = 0; j < NW; j++) {
+        const int n = tid / 8 + 32 * j, p = tid % 8;
+        s_w[((p / 2) * NT + n / 32) * 64 + n % 32 + 32 * (p % 2)] = wv[j];
+      }
+    } else if (tid < SQ) {
+      const int p = tid / (BN / VK);
+#pragma unroll
+      for (int c = 0; c < VK; c++) {
+        V v;
+#pragma unroll
+        for (int j = 0; j < VK; j++) v[j] = wv[j][c];
+        const int n = tid % (BN / VK) * VK + c;
+        s_w[((p / 2) * NT + n / 32) * 64 + n % 32 + 32 * (p % 2)] = v;
       }
     }
-    if (mine >= a.rows) continue;
-    TO *out = static_cast<TO *>(a.out) + r * a.ld_out;
+  };
+  f32x16 acc[2][NTW];
 #pragma unroll
-    for (int i = 0; i < NT; i++)
+  for (int i = 0; i < 2; i++)
+#pragma unroll
+    for (int n = 0; n < NTW; n++) acc[i][n] = f32x16{};
+  fetch(0);
+  put();
+  __syncthreads();
+  for (int k0 = 0; k0 < a.depth; k0 += KC) {
+    const bool more = k0 + KC < a.depth;
+    if (more) fetch(k0 + KC);
+#pragma unroll
+    for (int s = 0; s < 4; s++) {
+      V xs[2], ws[NTW];
+#pragma unroll
+      for (int i = 0; i < 2; i++) xs[i] = s_x[(wm * 64 + i * 32 + l % 32) * P + 2 * s + half];
+#pragma unroll
+      for (int n = 0; n < NTW; n++) ws[n] = s_w[(s * NT + wn * NTW + n) * 64 + l];
+      mma_block<T>(ws, xs, acc);
+    }
+    __syncthreads();
+    if (more) put();
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const int64_t r = m0 + wm * 64 + i * 32 + l % 32;
+    if (r >= a.rows) continue;
+#pragma unroll
+    for (int n = 0; n < NTW; n++)
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        const int c = n0 + i * 32 + 8 * e + 4 * half;
-        if (c >= a.width) continue;
-        float v[4] = {acc[i][4 * e], acc[i][4 * e + 1], acc[i][4 * e + 2], acc[i][4 * e + 3]};
-        if constexpr (!GRAD) {
-          if (a.bias) {
-            float b[4];
-            load4(static_cast<const T *>(a.bias), c, a.width, b);
+        const int c = n0 + (wn * NTW + n) * 32 + 8 * e + 4 * half;
+        float v[4] = {acc[i][n][4 * e], acc[i][n][4 * e + 1], acc[i][n][4 * e + 2], acc[i][n][4 * e + 3]};
+        if (c < a.width) finish4<T, TO, GRAD>(a, r, c, v);
+      }
+  }
+}
+
+// ------------------------------------------------------------------------------------ not many rows
+// 32 rows by 32 columns a workgroup, whose eight waves share the depth: where tiles of 128 rows would leave most of the card without work.
+// The fragments come straight from memory (W's columns, forward, element by element: 32 lanes side by side).
+constexpr int kSmallWaves = 8;
+template <class T, class TI, class TO, bool GRAD>
+__global__ __launch_bounds__(kWave * kSmallWaves) void k_linear_small(LinearArgs a) {
+  typedef typename Frag<T>::V V;
+  constexpr int VK = kVec<T>, KS = kStep<T>;
+  __shared__ float s_acc[kSmallWaves][32][36];
+  const int wave = threadIdx.x / kWave, l = lane_id(), half = l / 32;
+  const int64_t r0 = (int64_t)blockIdx.x * 32, r = min(r0 + l % 32, a.rows - 1);
+  const int n0 = blockIdx.y * 32, n = n0 + l % 32;
+  const T *w = static_cast<const T *>(a.weight);
+  f32x16 acc = f32x16{};
+#pragma unroll 2
+  for (int k0 = wave * KS; k0 < a.depth; k0 += kSmallWaves * KS) {
+    const int k = k0 + half * VK;
+    const V x = in_frag<T, TI, GRAD>(a, r, k);
+    V wv{};
+    if constexpr (GRAD) {
+      if (n < a.width) wv = row_frag<T>(w + (int64_t)n * a.ld_w, k, a.depth);
+    } else {
 #pragma unroll
-            for (int j = 0; j < 4; j++) v[j] += b[j];
-          }
-          if (a.keep) store4(static_cast<TO *>(a.keep) + r * a.ld_keep, c, a.width, v);
-          if (a.act != INK_ACT_NONE)
+      for (int j = 0; j < VK; j++)
+        if (n < a.width && k + j < a.depth) wv[j] = w[(int64_t)(k + j) * a.ld_w + n];
+    }
+    acc = mma(wv, x, acc);
+  }
 #pragma unroll
-            for (int j = 0; j < 4; j++) v[j] = activate(v[j], a.act);
-          if (a.res) {
-            float b[4];
-            load4(static_cast<const TO *>(a.res) + r * a.ld_res, c, a.width, b);
+  for (int e = 0; e < 4; e++) {
+    const F4 v = {acc[4 * e], acc[4 * e + 1], acc[4 * e + 2], acc[4 * e + 3]};
+    *reinterpret_cast<F4 *>(&s_acc[wave][l % 32][8 * e + 4 * half]) = v;
+  }
+  __syncthreads();
+  if (threadIdx.x >= 256) return;
+  const int row = threadIdx.x / 8, c = threadIdx.x % 8 * 4;
+  F4 t = F4{};
 #pragma unroll
-            for (int j = 0; j < 4; j++) v[j] += b[j];
+  for (int i = 0; i < kSmallWaves; i++) t += *reinterpret_cast<const F4 *>(&s_acc[i][row][c]);
+  float v[4] = {t[0], t[1], t[2], t[3]};
+  if (r0 + row < a.rows && n0 + c < a.width) finish4<T, TO, GRAD>(a, r0 + row, n0 + c, v);
+}
+
+// ------------------------------------------------------------------------------------ many rows
+// Rows in a stream.  A workgroup of WM x WN waves holds W in registers for good: a wave has the fragments of its 32 NTW columns over
+// the whole depth (KS steps).  It takes 32 WM rows at a time: all threads load them side by side (16 bytes a lane, whole lines), a tile
+// ahead, and put them into LDS, from where every wave reads the fragments of its 32 rows; the product goes through
+// LDS in 32 bits once more, so that residual, z and y are read and written in whole lines too.  What a row costs beyond its bytes is
+// then little LDS traffic and one matrix instruction per 32 x 32 x kStep.
+struct StreamArgs {
+  LinearArgs a;
+  int chunks, pitch, flat;                   // 16-byte pieces of a row's depth; floats between rows of results in LDS; see emit
+};
+
+// a piece of a row that starts `by` elements too early, moved down
+template <class V> __device__ __forceinline__ V move_down(V v, int by, int size) {
+  const unsigned __int128 u = __builtin_bit_cast(unsigned __int128, v) >> (8 * size * by);
+  return __builtin_bit_cast(V, u);
+}
+
+template <class T, class TI, class TO, int KS, int NTW, int WN, int WM, int WK, int PER, bool GRAD>
+__global__ __launch_bounds__(kWave * WN * WM * WK, PER) void k_linear_stream(StreamArgs sa) {
+  const LinearArgs &a = sa.a;
+  typedef typename Frag<T>::V V;
+  typedef typename Pack<TI, kVec<T>>::type In;
+  constexpr int VK = kVec<T>, THREADS = kWave * WN * WM * WK, MR = 32 * WM, NT = NTW * WN, BN = 32 * NT, STEPS = KS * WK;
+  constexpr int P = STEPS * 32 + 16;         // bytes between rows in LDS: 16 lanes' pieces fall on all banks
+  constexpr int NL = (MR * 2 * STEPS + THREADS - 1) / THREADS;
+  constexpr int OE = 16 / sizeof(TO), NO = (MR * BN / OE + THREADS - 1) / THREADS, PS = 4, PART = MR * (BN + 4);
+  static_assert(STEPS % PS == 0, "whole pieces");
+  extern __shared__ __align__(16) char s_mem[];
+  char *s_x = s_mem;
+  float *s_o = reinterpret_cast<float *>(s_mem + MR * P), *s_b = s_o + WK * PART;
+  const int tid = threadIdx.x, l = lane_id(), half = l / 32, wave = tid / kWave, wn = wave % WN, wm = wave / WN % WM, wk = wave / (WN * WM);
+  const int n0 = blockIdx.y * BN, width = min(BN, a.width - n0);
+  V w[KS][NTW];
+#pragma unroll
+  for (int k0 = 0; k0 < STEPS; k0 += PS) {
+    __syncthreads();
+    stage_weights<T, NT, GRAD>(a, reinterpret_cast<V *>(s_mem), k0 * kStep<T>, PS * kStep<T>, n0);
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < PS; s++)
+      if (WK == 1 || wk == (k0 + s) / KS)
+#pragma unroll
+        for (int i = 0; i < NTW; i++) w[(k0 + s) % KS][i] = reinterpret_cast<V *>(s_mem)[(s * NT + wn * NTW + i) * 64 + l];
+  }
+  __syncthreads();
+  for (int i = tid; i < MR * P / 16; i += THREADS) reinterpret_cast<V *>(s_x)[i] = V{};      // past the depth it stays zero
+  for (int i = tid; i < BN; i += THREADS) s_b[i] = !GRAD && a.bias && i < width ? (float)static_cast<const T *>(a.bias)[n0 + i] : 0.f;
+  const int64_t tiles = (a.rows + MR - 1) / MR;
+  const bool narrow = a.depth < VK;
+  // This thread's pieces of a tile of rows: place in LDS, and offsets from the tile's first row, the same for every tile.
+  In in[NL], pre[GRAD ? NL : 1];
+  int lds_at[NL];
+  uint32_t in_at[NL], pre_at[GRAD ? NL : 1];               // bytes
+  uint32_t tails = 0;                        // pieces that the end of the depth cuts
+#pragma unroll
+  for (int j = 0; j < NL; j++) {
+    const int i = min(tid + j * THREADS, MR * sa.chunks - 1);       // a thread without a piece repeats the last
+    const int row = i / sa.chunks, c = i - row * sa.chunks, at = narrow ? 0 : min(c * VK, a.depth - VK);
+    lds_at[j] = row * P + c * 16;
+    in_at[j] = (__umul24(row, (uint32_t)a.ld_in) + at) * (uint32_t)sizeof(TI);
+    if constexpr (GRAD) pre_at[j] = (__umul24(row, (uint32_t)a.ld_pre) + at) * (uint32_t)sizeof(TI);
+    if (c * VK + VK > a.depth) tails |= 1u << j;
+  }
+  auto load = [&](const TI *base, uint32_t at) -> In {     // a uniform base and 32 bits a lane: one register of address
+    const TI *x = reinterpret_cast<const TI *>(reinterpret_cast<const char *>(base) + at);
+    if (!narrow) return *reinterpret_cast<const In *>(x);
+    In v;
+#pragma unroll
+    for (int e = 0; e < VK; e++) v[e] = e < a.depth ? x[e] : (TI)0.f;
+    return v;
+  };
+  auto fetch = [&](int64_t t) {
+    const TI *x = static_cast<const TI *>(a.in) + t * MR * a.ld_in;
+    const TI *z = GRAD && a.pre ? static_cast<const TI *>(a.pre) + t * MR * a.ld_pre : nullptr;
+    const int64_t left = a.rows - t * MR;
+    if (left >= MR) {
+#pragma unroll
+      for (int j = 0; j < NL; j++) {
+        in[j] = load(x, in_at[j]);
+        if constexpr (GRAD) if (z) pre[j] = load(z, pre_at[j]);
+      }
+    } else {                                 // the last rows once more in place of those past the end
+#pragma unroll
+      for (int j = 0; j < NL; j++) {
+        const int row = lds_at[j] / P;
+        const uint32_t over = max(0, row - (int)left + 1) * (uint32_t)sizeof(TI);
+        in[j] = load(x, in_at[j] - over * (uint32_t)a.ld_in);
+        if constexpr (GRAD) if (z) pre[j] = load(z, pre_at[j] - over * (uint32_t)a.ld_pre);
+      }
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int j = 0; j < NL; j++) {
+      V v;
+      if constexpr (GRAD) {
+        float d[VK];
+#pragma unroll
+        for (int e = 0; e < VK; e++) d[e] = (float)in[j][e];
+        if (a.act != INK_ACT_NONE) {
+          float z[VK];
+#pragma unroll
+          for (int e = 0; e < VK; e++) z[e] = (float)pre[j][e];
+          scale_by_slope<VK>(d, z, a.act);
+        }
+#pragma unroll
+        for (int e = 0; e < VK; e++) v[e] = (T)d[e];
+      } else v = (V)in[j];
+      if (!narrow && (tails >> j & 1)) v = move_down(v, VK - a.depth % VK, sizeof(T));
+      *reinterpret_cast<V *>(s_x + lds_at[j]) = v;
+    }
+  };
+  // This thread's pieces of the results: 16 bytes of a row, or (flat: rows of an odd length that stand one behind the other) of the
+  // whole tile, which is then one row here.
+  typedef typename Pack<TO, OE>::type Out;
+  uint32_t out_row[NO];
+  int out_col[NO];
+  const int pieces = (width + OE - 1) / OE;
+#pragma unroll
+  for (int j = 0; j < NO; j++) {
+    const int i = tid + j * THREADS;
+    out_row[j] = sa.flat ? 0 : i / pieces;
+    out_col[j] = (sa.flat ? i : i - (int)out_row[j] * pieces) * OE;
+  }
+  auto place = [&](auto *base, int64_t ld, int j) {
+    typedef std::conditional_t<std::is_const_v<std::remove_pointer_t<decltype(base)>>, const char, char> Byte;
+    return reinterpret_cast<decltype(base)>(reinterpret_cast<Byte *>(base) + (__umul24(out_row[j], (uint32_t)ld) + out_col[j]) * (uint32_t)sizeof(TO));
+  };
+  int64_t t = blockIdx.x;
+  if (t < tiles) fetch(t);
+  __syncthreads();                           // the zeros are there
+  for (; t < tiles; t += gridDim.x) {
+    put();
+    __syncthreads();
+    if (t + gridDim.x < tiles) fetch(t + gridDim.x);
+    const int rows = (int)min((int64_t)MR, a.rows - t * MR);
+    const int row_n = sa.flat ? 1 : rows, col_n = sa.flat ? rows * width : width;
+    Out res[GRAD ? 1 : NO];
+    if constexpr (!GRAD)
+      if (a.res) {
+        const TO *q = static_cast<const TO *>(a.res) + t * MR * a.ld_res + n0;
+#pragma unroll
+        for (int j = 0; j < NO; j++)
+          if ((int)out_row[j] < row_n && out_col[j] + OE <= col_n) res[j] = *reinterpret_cast<const Out *>(place(q, a.ld_res, j));
+      }
+    f32x16 acc[NTW];
+#pragma unroll
+    for (int i = 0; i < NTW; i++) acc[i] = f32x16{};
+    const char *xs = s_x + (wm * 32 + l % 32) * P + wk * (KS * 32) + half * 16;
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
+      const V x = *reinterpret_cast<const V *>(xs + k * 32);
+#pragma unroll
+      for (int i = 0; i < NTW; i++) acc[i] = mma(w[k][i], x, acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NTW; i++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const int c = (wn * NTW + i) * 32 + 8 * e + 4 * half;
+        F4 v = {acc[i][4 * e], acc[i][4 * e + 1], acc[i][4 * e + 2], acc[i][4 * e + 3]};
+        if constexpr (!GRAD)
+          if (wk == 0) v += *reinterpret_cast<const F4 *>(s_b + c);
+        float *o = s_o + wk * PART + (wm * 32 + l % 32) * sa.pitch + c;
+        if (!sa.flat) *reinterpret_cast<F4 *>(o) = v;
+        else
+#pragma unroll
+          for (int j = 0; j < 4; j++)
+            if (c + j < width) o[j] = v[j];
+      }
+    __syncthreads();
+    TO *to = static_cast<TO *>(a.out) + t * MR * a.ld_out + n0;
+    TO *keep = !GRAD && a.keep ? static_cast<TO *>(a.keep) + t * MR * a.ld_keep + n0 : nullptr;
+#pragma unroll
+    for (int j = 0; j < NO; j++) {
+      if ((int)out_row[j] >= row_n || out_col[j] >= col_n) continue;
+      const F4 *o = reinterpret_cast<const F4 *>(s_o + ((int)__umul24(out_row[j], (uint32_t)sa.pitch) + out_col[j]));
+      float v[OE];
+#pragma unroll
+      for (int e = 0; e < OE; e++) v[e] = o[e / 4][e % 4];
+#pragma unroll
+      for (int q = 1; q < WK; q++)           // the parts of the depth, in order
+#pragma unroll
+        for (int e = 0; e < OE; e++) v[e] += o[q * (PART / 4) + e / 4][e % 4];
+      const bool whole = out_col[j] + OE <= col_n;
+      if constexpr (!GRAD) {
+        if (keep && whole) store_pack<TO, OE>(place(keep, a.ld_keep, j), v);
+        if (keep && !whole)
+#pragma unroll
+          for (int e = 0; e < OE; e++)
+            if (out_col[j] + e < col_n) place(keep, a.ld_keep, j)[e] = (TO)v[e];
+        activate_all<OE>(v, a.act);
+        if (a.res) {
+          if (whole)
+#pragma unroll
+            for (int e = 0; e < OE; e++) v[e] += (float)res[j][e];
+          else {
+            const TO *q = place(static_cast<const TO *>(a.res) + t * MR * a.ld_res + n0, a.ld_res, j);
+#pragma unroll
+            for (int e = 0; e < OE; e++)
+              if (out_col[j] + e < col_n) v[e] += (float)q[e];
           }
         }
-        store4(out, c, a.width, v);
       }
+      if (whole) store_pack<TO, OE>(place(to, a.ld_out, j), v);
+      else
+#pragma unroll
+        for (int e = 0; e < OE; e++)
+          if (out_col[j] + e < col_n) place(to, a.ld_out, j)[e] = (TO)v[e];
+    }
   }
 }
 
@@ -385,39 +754,68 @@ __global__ __launch_bounds__(kHeadThreads) void k_weight_sum(const float *part, 
 
 // ------------------------------------------------------------------------------------ host side
 constexpr int64_t kFewRows = 16;
-constexpr int kWeightLds = 64 << 10;
-
-// tiles of 32 columns a workgroup takes: all columns up to eight tiles, fewer where that leaves the card empty
-static int linear_tiles(int64_t rows, int width) {
-  const int all = (width + 31) / 32;
-  int nt = all >= 8 ? 8 : all > 6 ? 8 : all > 4 ? 6 : all > 2 ? 4 : 2;
-  while (nt > 2 && (rows + 255) / 256 * ((all + nt - 1) / nt) < 256) nt = nt == 6 ? 4 : nt / 2;
-  return nt;
-}
-
-template <class T, class TI, class TO, int NT, bool GRAD> static void linear_launch(LinearArgs a, Launches &run) {
-  constexpr int KS = kStep<T>;
-  const int padded = (a.depth + KS - 1) / KS * KS, most = kWeightLds / (NT * 32 * (int)sizeof(T)) / KS * KS;
-  a.chunk = std::min(padded, most);
-  const int lds = a.chunk * NT * 32 * (int)sizeof(T);
-  const int threads = a.rows <= 128 * 256 ? 256 : kLinearThreads;
-  const int64_t tile = threads / 2;
-  const unsigned gy = (unsigned)((a.width + NT * 32 - 1) / (NT * 32));
-  const int64_t tiles = (a.rows + tile - 1) / tile;
-  const int64_t most_x = a.chunk >= a.depth ? std::max<int64_t>(1, 1024 / gy) : tiles;
+template <class T, class TI, class TO, int KS, int NTW, int WN, int WM, int WK, int PER, bool GRAD>
+static void stream_launch(const LinearArgs &a, Launches &run) {
+  constexpr int MR = 32 * WM, BN = 32 * NTW * WN, OE = 16 / (int)sizeof(TO), WAVES = WN * WM * WK;
+  StreamArgs s{a, (a.depth + kVec<T> - 1) / kVec<T>, BN + 4, 0};
+  s.flat = a.width <= BN && a.width % OE != 0 && a.ld_out == a.width && (!a.keep || a.ld_keep == a.width) && (!a.res || a.ld_res == a.width);
+  if (s.flat) s.pitch = a.width;
+  const unsigned gy = (unsigned)((a.width + BN - 1) / BN);
+  const int64_t tiles = (a.rows + MR - 1) / MR;
+  constexpr int lds = MR * (KS * WK * 32 + 16) + WK * MR * (BN + 4) * 4 + BN * 4;
+  static_assert(lds <= 160 << 10 && lds >= 4 * BN * 32, "LDS holds the tiles, and W's pieces on their way to the registers");
+  constexpr int per_cu = std::max(1, std::min((160 << 10) / lds, 4 * PER / WAVES));
   run.lds = lds;
-  run(k_linear<T, TI, TO, NT, GRAD>, dim3((unsigned)std::min(tiles, most_x), gy), dim3(threads), a);
+  run(k_linear_stream<T, TI, TO, KS, NTW, WN, WM, WK, PER, GRAD>, dim3((unsigned)std::min<int64_t>(tiles, std::max(1u, 256 * per_cu / gy)), gy),
+      dim3(kWave * WAVES), s);
   run.lds = 0;
 }
+// whether the rows are so many that a workgroup takes several tiles, and W fits the registers
+template <class T, class TI, class TO, bool GRAD> static bool stream_run(const LinearArgs &a, Launches &run) {
+  if (a.rows < 32 * 1024) return false;
+  for (const int64_t ld : {a.ld_in, a.ld_pre, a.ld_res, a.ld_out, a.ld_keep})
+    if (ld >= 1 << 22) return false;         // offsets within a tile are 32-bit
+  const int steps = (a.depth + kStep<T> - 1) / kStep<T>;
+  if constexpr (sizeof(T) == 2) {
+    if (steps <= 8) {
+      if (a.width <= 64) stream_launch<T, TI, TO, 8, 1, 2, 2, 1, 2, GRAD>(a, run);
+      else if (a.width <= 128) stream_launch<T, TI, TO, 8, 2, 2, 2, 1, 2, GRAD>(a, run);
+      else stream_launch<T, TI, TO, 8, 2, 4, 1, 1, 2, GRAD>(a, run);
+    } else if (steps <= 16) {
+      if (a.width <= 64) stream_launch<T, TI, TO, 8, 1, 2, 1, 2, 4, GRAD>(a, run);
+      else if (a.width <= 128) stream_launch<T, TI, TO, 16, 1, 4, 1, 1, 2, GRAD>(a, run);
+      else stream_launch<T, TI, TO, 16, 1, 8, 1, 1, 2, GRAD>(a, run);
+    } else if (steps <= 40) {
+      if (a.width <= 64) stream_launch<T, TI, TO, 10, 1, 2, 1, 4, 2, GRAD>(a, run);
+      else if (a.width <= 128) stream_launch<T, TI, TO, 20, 1, 4, 1, 2, 2, GRAD>(a, run);
+      else stream_launch<T, TI, TO, 40, 1, 8, 1, 1, 2, GRAD>(a, run);
+    } else return false;
+  } else {
+    if (steps <= 16) {
+      if (a.width <= 64) stream_launch<T, TI, TO, 8, 1, 2, 1, 2, 4, GRAD>(a, run);
+      else if (a.width <= 128) stream_launch<T, TI, TO, 16, 1, 4, 1, 1, 2, GRAD>(a, run);
+      else stream_launch<T, TI, TO, 16, 1, 8, 1, 1, 2, GRAD>(a, run);
+    } else if (steps <= 32) {
+      if (a.width <= 64) stream_launch<T, TI, TO, 16, 1, 2, 1, 2, 2, GRAD>(a, run);
+      else if (a.width <= 128) stream_launch<T, TI, TO, 16, 1, 4, 1, 2, 2, GRAD>(a, run);
+      else stream_launch<T, TI, TO, 32, 1, 8, 1, 1, 2, GRAD>(a, run);
+    } else return false;
+  }
+  return true;
+}
+
 template <class T, class TI, class TO, bool GRAD> static void linear_run(const LinearArgs &a, Launches &run) {
   if constexpr (!GRAD)
     if (a.rows <= kFewRows) return run(k_linear_few<T, TO>, dim3((a.width + 31) / 32, (unsigned)a.rows), dim3(kHeadThreads), a);
-  switch (linear_tiles(a.rows, a.width)) {
-    case 2: return linear_launch<T, TI, TO, 2, GRAD>(a, run);
-    case 4: return linear_launch<T, TI, TO, 4, GRAD>(a, run);
-    case 6: return linear_launch<T, TI, TO, 6, GRAD>(a, run);
-    default: return linear_launch<T, TI, TO, 8, GRAD>(a, run);
+  if (stream_run<T, TI, TO, GRAD>(a, run)) return;
+  const int64_t tiles = (a.rows + 127) / 128;
+  const int ntw = a.width <= 64 ? 1 : 2, gy = (a.width + 64 * ntw - 1) / (64 * ntw);
+  if (tiles * gy < 256) {
+    const dim3 grid((unsigned)((a.rows + 31) / 32), (a.width + 31) / 32);
+    return run(k_linear_small<T, TI, TO, GRAD>, grid, dim3(kWave * kSmallWaves), a);
   }
+  const dim3 grid((unsigned)((tiles + 7) / 8 * 8 * gy));
+  run(ntw == 1 ? k_linear_tile<T, TI, TO, 1, GRAD> : k_linear_tile<T, TI, TO, 2, GRAD>, grid, dim3(256), a);
 }
 
 struct GradPlan { int kt, nt, slices; int64_t slice; };

@@ -231,6 +231,53 @@ def test_linear(rows, cols, out, dtype):
         assert torch.equal(y, y2), "the layout of the tensors changed the result"
 
 
+# enough rows for the kernels that keep W in registers, or for their fallback (deep sums): every class of depth and width, sizes beside
+# the tiles', a last tile of one row
+MANY = [(32769, 128, 47), (33000, 100, 64), (32800, 128, 128), (32769, 64, 172), (32768, 200, 41), (32790, 256, 256), (32769, 255, 100), (32801, 300, 47),
+        (32769, 602, 128), (33001, 602, 256), (32769, 640, 300), (32769, 7, 9), (33333, 3, 5), (32769, 650, 70), (32777, 33, 1)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,out", MANY)
+def test_linear_many_rows(rows, cols, out, dtype):
+    g, x, w, b = linear_case(rows, cols, out, dtype, rows + 7 * cols + out)
+    r = torch.randn(rows, out, generator=g)
+    for act, res, bias, f32, pad in (("gelu", True, True, False, 0), ("relu", True, False, True, 5), ("silu", False, True, False, 2)):
+        to = F32 if f32 else dtype
+        rr = r.to(to) if res else None
+        args = (b.cuda() if bias else None, act, None if rr is None else table(rr, out + pad, pad))
+        y, z = head.linear(table(x, cols + pad, pad), table(w, out + pad, pad), *args, keep_pre=True, out_dtype=to)
+        want = linear_ref(x, w, b if bias else None, act, rr)
+        close(z, want[1], want[3], to, "z " + act)
+        close(y, want[0], want[2], to, "y " + act)
+        assert torch.equal(y, head.linear(x.cuda(), w.cuda(), *args, out_dtype=to))
+    view = torch.full((rows, out + 9), 7.0, dtype=dtype, device="cuda")       # results as columns of a wider table: nothing beside them is written
+    wide = table(x)
+    lib, stream = head._functions(), torch.cuda.current_stream().cuda_stream
+    wd = w.cuda()
+    assert lib.ink_linear(wide.data_ptr(), cols, wd.data_ptr(), out, None, None, 0, rows, cols, out, head.TYPES[dtype], head.TYPES[dtype], 0,
+                          view[:, 4:].data_ptr(), out + 9, None, 0, stream) == 0
+    torch.cuda.synchronize()
+    want = linear_ref(x, w, None, "none", None)
+    close(view[:, 4:4 + out], want[0], want[2], dtype, "columns of a table")
+    assert (view[:, :4] == 7).all() and (view[:, 4 + out:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,out", MANY)
+def test_linear_backward_many_rows(rows, cols, out, dtype):
+    g, x, w, _ = linear_case(rows, cols, out, dtype, rows * 5 + cols + out)
+    dy, pre = torch.randn(rows, out, generator=g), 2 * torch.randn(rows, out, generator=g)
+    for act, f32, pad in (("none", False, 1), ("gelu", True, 0), ("silu", False, 4)):
+        to = F32 if f32 and dtype == BF16 else dtype
+        d, p = dy.to(to), pre.to(to)
+        got = head.linear_backward(table(d, out + pad, pad), table(x, cols + pad, pad), table(w, out + pad, pad),
+                                   pre=None if act == "none" else table(p, out + 2 * pad, pad), act=act)
+        want = linear_grad_ref(d, x, w, p, act, dtype)
+        for i, name in enumerate(("dx", "dweight", "dbias")):
+            close(got[i], want[i], want[3 + i], dtype, name + " " + act)
+
+
 def linear_grad_ref(dy, x, w, pre, act, dtype):
     dz = dy.double()
     e = torch.zeros_like(dz)
