@@ -632,124 +632,282 @@ __global__ __launch_bounds__(kHeadThreads) void k_linear_few(LinearArgs a) {
   static_cast<TO *>(a.out)[r * a.ld_out + c] = (TO)v;
 }
 
-// ------------------------------------------------------------------------------------ gradient of the weights
-struct WeightGradArgs {
-  const void *x, *dy, *pre;
-  float *part, *part_bias;                   // [slices][cols][out], [slices][out]
-  int64_t rows, ld_x, ld_dy, ld_pre, slice;  // rows of a slice
+// ------------------------------------------------------------------------------------ gradient
+// dweight = x^T dz and dbias over a slice of the rows, and (DX) dx = dz W^T of its rows on the way, so that dy, z and x are read once.
+// A workgroup has the sums of 32 KT columns of x by 32 NT of dz in registers, (KT / 2) (NT / 2) tiles a wave, and takes 32 rows at a time, one
+// piece ahead in registers.  All threads load x, dy and z side by side, 16 bytes a lane, form dz once and put both into LDS row by row.  The
+// sums run over the rows, so their fragments are columns: 16-bit ones come from the transposing LDS read, 32-bit ones element by
+// element.  The partial sums are left in the fragments' order and k_grad_sum puts them where they belong.
+struct GradArgs {
+  const void *x, *dy, *pre, *weight;
+  void *dx;
+  float *part, *part_bias;                   // fragments of [slices][tiles][KT][NT], or NULL; [slices][32 NT tiles], or NULL
+  int64_t rows, ld_x, ld_dy, ld_pre, ld_w, ld_dx, slice;
   int cols, out, act;
 };
+constexpr int kGradRows = 32, kGradThreads = 256;
 
-constexpr int kGradRows = 64;                // rows in LDS at a time
+// Bytes between rows in LDS: rows of 16 lanes' pieces fall on all banks, and in 32 bits two rows side by side nearly so.
+template <class T, int TILES> constexpr int kGradPitch = TILES * 32 * (int)sizeof(T) + (sizeof(T) == 2 ? 16 : 144);
 
-// Squares of VK rows x VK columns, transposed in registers: fragment (step, tile) holds 32 columns of 2 VK rows, a lane VK rows of a column.
-// `get(row, column)` gives VK elements of a row.
-template <class T, int NT, class Get> __device__ __forceinline__ void stage_rows(typename Frag<T>::V *s, Get get) {
-  constexpr int VK = kVec<T>, NB = NT * 32 / VK, RB = kGradRows / VK;
-  for (int i = threadIdx.x; i < NB * RB; i += kLinearThreads) {
-    const int nb = i % NB, rb = i / NB;
-    typename Frag<T>::V rows[VK];
+// Fragment of a step (2 kVec rows) of 32 columns of rows in LDS.  16 bits: of 16 lanes, lane 4 j + b gives the place of columns 4 b .. of
+// row j, and lane i gets column i of the four rows.  Which rows of a step a lane holds is the same for both operands, and nothing else matters.
+template <class T> __device__ __forceinline__ typename Frag<T>::V columns_frag(const char *rows, int pitch, int step, int tile) {
+  const int l = lane_id(), half = l / 32;
+  if constexpr (sizeof(T) == 2) {
+    typedef short S4 __attribute__((ext_vector_type(4)));
+    typedef S4 __attribute__((address_space(3))) *Lds;
+    const char *at = rows + (step * 16 + half * 8 + l % 16 / 4) * pitch + (tile * 32 + l / 16 % 2 * 16 + l % 4 * 4) * 2;
+    const S4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * pitch));
+    typedef short S8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(typename Frag<T>::V, (S8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    typename Frag<T>::V v;
 #pragma unroll
-    for (int j = 0; j < VK; j++) rows[j] = get(rb * VK + j, nb * VK);
-#pragma unroll
-    for (int c = 0; c < VK; c++) {
-      typename Frag<T>::V v;
-#pragma unroll
-      for (int j = 0; j < VK; j++) v[j] = rows[j][c];
-      const int col = nb * VK + c;
-      s[((rb / 2) * NT + col / 32) * 64 + col % 32 + 32 * (rb % 2)] = v;
-    }
+    for (int j = 0; j < 4; j++) v[j] = *reinterpret_cast<const float *>(rows + (step * 8 + 2 * j + half) * pitch + (tile * 32 + l % 32) * 4);
+    return v;
   }
 }
 
-// Tile of 32 KT columns of x by 32 NT columns of dz over a slice of the rows.  Eight waves: wave w has x tiles w % KW ..
-template <class T, class TI, int KT, int NT>
-__global__ __launch_bounds__(kLinearThreads) void k_weight_grad(WeightGradArgs a) {
+template <class T, class TI, int KT, int NT, bool DX>
+__global__ __launch_bounds__(kGradThreads, 2) void k_linear_grad(GradArgs a) {
   typedef typename Frag<T>::V V;
-  constexpr int W = kLinearThreads / kWave, KW = KT < W ? KT : W, NW = W / KW, KP = KT / KW, NP = (NT + NW - 1) / NW;
-  constexpr int STEPS = kGradRows / kStep<T>;
-  __shared__ V s_x[STEPS * KT * 64], s_z[STEPS * NT * 64];
-  const int w = threadIdx.x / kWave, l = lane_id();
-  const int kt0 = (w % KW) * KP, nt0 = (w / KW) * NP;
+  constexpr int VK = kVec<T>, STEPS = kGradRows / kStep<T>, CX = KT * 32 / VK, CZ = NT * 32 / VK;      // pieces of a row
+  constexpr int NX = kGradRows * CX / kGradThreads, NZ = kGradRows * CZ / kGradThreads;
+  constexpr int KP = KT / 2, NP = NT / 2, DP = (KT + 3) / 4, DS = CZ / 2;      // tiles a wave; column tiles of dx a wave, steps of its depth
+  constexpr int PX = kGradPitch<T, KT>, PZ = kGradPitch<T, NT>, PD = KT * 32 + 4, PB = NT * 32 + 4;
+  constexpr int kLds = kGradRows * (PX + PZ + (DX ? PD * 4 : 0)), kLdsBias = kGradRows * PB * 4;
+  __shared__ __align__(16) char s_mem[kLds > kLdsBias ? kLds : kLdsBias];
+  __shared__ __align__(16) float s_db[NZ * VK > 16 ? kGradRows * PB : 1];
+  char *s_x = s_mem, *s_z = s_mem + kGradRows * PX;
+  float *s_dx = reinterpret_cast<float *>(s_z + kGradRows * PZ);
+  const int tid = threadIdx.x, l = lane_id(), half = l / 32, wave = tid / kWave;
   const int k0 = blockIdx.x * (KT * 32), n0 = blockIdx.y * (NT * 32);
   const int64_t r_begin = blockIdx.z * a.slice, r_end = min(r_begin + a.slice, a.rows);
+  const int x_cols = a.x ? a.cols : 0;
+  V w[DX ? DP : 1][DX ? DS : 1];
+  if constexpr (DX)
+#pragma unroll
+    for (int i = 0; i < DP; i++)
+#pragma unroll
+      for (int s = 0; s < DS; s++) {
+        const int k = (wave + 4 * i) * 32 + l % 32, n = s * kStep<T> + half * VK;
+        w[i][s] = V{};
+        if (k < a.cols && n < a.out) w[i][s] = row_frag<T>(static_cast<const T *>(a.weight) + (int64_t)k * a.ld_w, n, a.out);
+      }
   f32x16 acc[KP][NP];
 #pragma unroll
   for (int i = 0; i < KP; i++)
 #pragma unroll
     for (int j = 0; j < NP; j++) acc[i][j] = f32x16{};
+  // Eight threads share a row: pieces tid % 8, + 8, ... of row tid / 8.  A piece that the matrix's end cuts starts earlier and is moved
+  // down; one past it, or of a row past the slice, is not loaded and put down as zero.
+  typedef typename Pack<T, VK>::type PT;
+  typedef typename Pack<TI, VK>::type PI;
+  const int my_row = tid / 8, my_piece = tid % 8;
+  const T *xp = static_cast<const T *>(a.x) + (a.x ? (r_begin + my_row) * a.ld_x : 0);
+  const TI *yp = static_cast<const TI *>(a.dy) + (r_begin + my_row) * a.ld_dy, *zp = static_cast<const TI *>(a.pre) + (a.pre ? (r_begin + my_row) * a.ld_pre : 0);
+  PT x[NX];
+  PI dy[NZ], pre[NZ];
+  // Column sums of dz: in registers, or, where those are wanted elsewhere, in LDS, each place this thread's own.
+  constexpr bool DB_LDS = NZ * VK > 16;
+  float db[DB_LDS ? 1 : NZ][VK];
+#pragma unroll
+  for (int j = 0; j < NZ; j++)
+#pragma unroll
+    for (int e = 0; e < VK; e++) {
+      if constexpr (DB_LDS) s_db[my_row * PB + (my_piece + 8 * j) * VK + e] = 0.f;
+      else db[j][e] = 0.f;
+    }
+  auto load = [&](auto *row, int c, int n) {
+    typedef std::remove_const_t<std::remove_pointer_t<decltype(row)>> E;
+    typedef typename Pack<E, VK>::type P;
+    if (n >= VK) return *reinterpret_cast<const P *>(row + min(c, n - VK));
+    P v;
+#pragma unroll
+    for (int e = 0; e < VK; e++) v[e] = e < n ? row[e] : (E)0.f;
+    return v;
+  };
+  auto fetch = [&](int64_t left) {           // rows left in the slice
+    if (my_row < left) {
+#pragma unroll
+      for (int j = 0; j < NX; j++) {
+        const int c = k0 + (my_piece + 8 * j) * VK;
+        if (c < x_cols) x[j] = load(xp, c, x_cols);
+      }
+#pragma unroll
+      for (int j = 0; j < NZ; j++) {
+        const int c = n0 + (my_piece + 8 * j) * VK;
+        if (c < a.out) {
+          dy[j] = load(yp, c, a.out);
+          if (a.act != INK_ACT_NONE) pre[j] = load(zp, c, a.out);
+        }
+      }
+    }
+    xp += kGradRows * a.ld_x;
+    yp += kGradRows * a.ld_dy;
+    zp += kGradRows * a.ld_pre;
+  };
+  auto put = [&](int64_t left) {
+#pragma unroll
+    for (int j = 0; j < NX; j++) {
+      const int c = k0 + (my_piece + 8 * j) * VK;
+      V v{};
+      if (my_row < left && c < x_cols) {
+        v = (V)x[j];
+        if (c + VK > x_cols && x_cols >= VK) v = move_down(v, c + VK - x_cols, sizeof(T));
+      }
+      *reinterpret_cast<V *>(s_x + my_row * PX + (my_piece + 8 * j) * 16) = v;
+    }
+#pragma unroll
+    for (int j = 0; j < NZ; j++) {
+      const int c = n0 + (my_piece + 8 * j) * VK;
+      V v{};
+      if (my_row < left && c < a.out) {
+        float d[VK];
+#pragma unroll
+        for (int e = 0; e < VK; e++) d[e] = (float)dy[j][e];
+        if (a.act != INK_ACT_NONE) {
+          float z[VK];
+#pragma unroll
+          for (int e = 0; e < VK; e++) z[e] = (float)pre[j][e];
+          scale_by_slope<VK>(d, z, a.act);
+        }
+#pragma unroll
+        for (int e = 0; e < VK; e++) {
+          if constexpr (DB_LDS) s_db[my_row * PB + (my_piece + 8 * j) * VK + e] += d[e];
+          else db[j][e] += d[e];
+          v[e] = (T)d[e];
+        }
+        if (c + VK > a.out && a.out >= VK) v = move_down(v, c + VK - a.out, sizeof(T));
+      }
+      *reinterpret_cast<V *>(s_z + my_row * PZ + (my_piece + 8 * j) * 16) = v;
+    }
+  };
+  if (r_begin < r_end) fetch(r_end - r_begin);
   for (int64_t r0 = r_begin; r0 < r_end; r0 += kGradRows) {
+    put(r_end - r0);
     __syncthreads();
-    stage_rows<T, KT>(s_x, [&](int r, int c) {
-      V v{};
-      if (r0 + r < r_end && k0 + c < a.cols) v = row_frag<T>(static_cast<const T *>(a.x) + (r0 + r) * a.ld_x, k0 + c, a.cols);
-      return v;
-    });
-    stage_rows<T, NT>(s_z, [&](int r, int c) {
-      V v{};
-      if (r0 + r < r_end && n0 + c < a.out)
-        v = grad_frag<T, TI>(static_cast<const TI *>(a.dy) + (r0 + r) * a.ld_dy,
-                             static_cast<const TI *>(a.pre) + (a.pre ? (r0 + r) * a.ld_pre : 0), n0 + c, a.out, a.act);
-      return v;
-    });
-    __syncthreads();
+    if (r0 + kGradRows < r_end) fetch(r_end - r0 - kGradRows);
 #pragma unroll
     for (int s = 0; s < STEPS; s++) {
-      V z[NP];
+      V zs[NP], xs[KP];
 #pragma unroll
-      for (int j = 0; j < NP; j++) z[j] = s_z[(s * NT + min(nt0 + j, NT - 1)) * 64 + l];
+      for (int j = 0; j < NP; j++) zs[j] = columns_frag<T>(s_z, PZ, s, wave / 2 * NP + j);
 #pragma unroll
-      for (int i = 0; i < KP; i++) {
-        const V x = s_x[(s * KT + kt0 + i) * 64 + l];
+      for (int i = 0; i < KP; i++) xs[i] = columns_frag<T>(s_x, PX, s, wave % 2 * KP + i);
+      mma_block<T>(zs, xs, acc);
+    }
+    if constexpr (DX) {
 #pragma unroll
-        for (int j = 0; j < NP; j++) acc[i][j] = mma(z[j], x, acc[i][j]);
+      for (int i = 0; i < DP; i++) {
+        if (wave + 4 * i >= KT) continue;
+        f32x16 d = f32x16{};
+#pragma unroll
+        for (int s = 0; s < DS; s++) d = mma(w[i][s], *reinterpret_cast<const V *>(s_z + l % 32 * PZ + (2 * s + half) * 16), d);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const F4 v = {d[4 * e], d[4 * e + 1], d[4 * e + 2], d[4 * e + 3]};
+          *reinterpret_cast<F4 *>(s_dx + (l % 32) * PD + (wave + 4 * i) * 32 + 8 * e + 4 * half) = v;
+        }
+      }
+    }
+    __syncthreads();
+    if constexpr (DX) {
+      const int rows = (int)min((int64_t)kGradRows, r_end - r0);
+#pragma unroll
+      for (int j = 0; j < NX; j++) {
+        const int c = (my_piece + 8 * j) * VK;
+        if (my_row >= rows || c >= a.cols) continue;
+        const F4 *o = reinterpret_cast<const F4 *>(s_dx + my_row * PD + c);
+        T *to = static_cast<T *>(a.dx) + (r0 + my_row) * a.ld_dx + c;
+        float v[VK];
+#pragma unroll
+        for (int e = 0; e < VK; e++) v[e] = o[e / 4][e % 4];
+        if (c + VK <= a.cols) store_pack<T, VK>(to, v);
+        else
+#pragma unroll
+          for (int e = 0; e < VK; e++)
+            if (c + e < a.cols) to[e] = (T)v[e];
       }
     }
   }
-  float *part = a.part + (int64_t)blockIdx.z * a.cols * a.out;
+  const int64_t tile = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * gridDim.y + blockIdx.y;
+  if (a.part) {
+    float *part = a.part + tile * (KT * NT * 1024);
 #pragma unroll
-  for (int i = 0; i < KP; i++)
+    for (int i = 0; i < KP; i++)
 #pragma unroll
-    for (int j = 0; j < NP; j++) {
-      const int k = k0 + (kt0 + i) * 32 + l % 32;
-      if (k >= a.cols || nt0 + j >= NT) continue;
+      for (int j = 0; j < NP; j++)
 #pragma unroll
-      for (int e = 0; e < 4; e++) {
-        const int c = n0 + (nt0 + j) * 32 + 8 * e + 4 * (l / 32);
-        const float v[4] = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
-        if (c < a.out) store4(part + (int64_t)k * a.out, c, a.out, v);
-      }
+        for (int e = 0; e < 4; e++) {
+          const F4 v = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+          reinterpret_cast<F4 *>(part)[(((wave % 2 * KP + i) * NT + wave / 2 * NP + j) * 4 + e) * 64 + l] = v;
+        }
+  }
+  if (!a.part_bias || blockIdx.x) return;
+  // column sums of dz: each thread's of its row's pieces, over the 32 rows.  A moved piece's first columns belong to the one before.
+  float *s_sum = DB_LDS ? s_db : reinterpret_cast<float *>(s_mem);           // [32][PB]
+  float own[NZ][VK];
+#pragma unroll
+  for (int j = 0; j < NZ; j++)
+#pragma unroll
+    for (int e = 0; e < VK; e++) {
+      if constexpr (DB_LDS) own[j][e] = s_db[my_row * PB + (my_piece + 8 * j) * VK + e];
+      else own[j][e] = db[j][e];
     }
-}
-
-// column sums of dz over a slice of the rows: 64 columns a workgroup, a wave takes every fourth row
-template <class TI> __global__ __launch_bounds__(kHeadThreads) void k_bias_grad(WeightGradArgs a) {
-  constexpr int W = kHeadThreads / kWave;
-  __shared__ float s_sum[W][kWave];
-  const int w = threadIdx.x / kWave, c = blockIdx.x * kWave + lane_id();
-  const int64_t r_begin = blockIdx.y * a.slice, r_end = min(r_begin + a.slice, a.rows);
-  float t = 0.f;
-  if (c < a.out)
-    for (int64_t r = r_begin + w; r < r_end; r += W) {
-      const float d = (float)static_cast<const TI *>(a.dy)[r * a.ld_dy + c];
-      t += a.act != INK_ACT_NONE ? d * activate_grad((float)static_cast<const TI *>(a.pre)[r * a.ld_pre + c], a.act) : d;
-    }
-  s_sum[w][lane_id()] = t;
   __syncthreads();
-  if (w || c >= a.out) return;
-  t = 0.f;
 #pragma unroll
-  for (int i = 0; i < W; i++) t += s_sum[i][lane_id()];
-  a.part_bias[(int64_t)blockIdx.y * a.out + c] = t;
+  for (int j = 0; j < NZ; j++) {
+    const int cb = my_piece + 8 * j, c = n0 + cb * VK, over = c + VK > a.out && a.out >= VK ? c + VK - a.out : 0;
+#pragma unroll
+    for (int e = 0; e < VK; e++)
+      if (c < a.out && e >= over && c - over + e < a.out) s_sum[my_row * PB + cb * VK + e - over] = own[j][e];
+  }
+  __syncthreads();
+  for (int c = tid; c < NT * 32; c += kGradThreads) {
+    if (n0 + c >= a.out) continue;
+    float t = 0.f;
+#pragma unroll
+    for (int r = 0; r < kGradRows; r++) t += s_sum[r * PB + c];
+    a.part_bias[((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * (NT * 32) + c] = t;
+  }
 }
 
-// partial sums of n elements from `slices` slices to their sum
-__global__ __launch_bounds__(kHeadThreads) void k_weight_sum(const float *part, int64_t n, int slices, int type, int out, void *to, int64_t ld_to) {
-  const int64_t i = (int64_t)blockIdx.x * kHeadThreads + threadIdx.x;
-  if (i >= n) return;
-  float t = 0.f;
-  for (int s = 0; s < slices; s++) t += part[s * n + i];
-  store_any(to, i / out * ld_to + i % out, type, t);
+// Partial sums of all slices: 64 elements, four by four, a workgroup; 16 threads share a sum.  The last workgroups do the bias.
+struct GradSumArgs {
+  const float *part, *part_bias;
+  void *dweight, *dbias;
+  int64_t ld_dw;
+  int slices, type, cols, out, kt, nt, tiles_k, tiles_n, weight_groups;
+};
+__global__ __launch_bounds__(256) void k_grad_sum(GradSumArgs a) {
+  __shared__ F4 s[16][17];
+  const int x = threadIdx.x % 16, y = threadIdx.x / 16;
+  const bool bias = (int)blockIdx.x >= a.weight_groups;
+  const int64_t n = bias ? (int64_t)a.tiles_n * a.nt * 32 : (int64_t)a.tiles_k * a.tiles_n * a.kt * a.nt * 1024;
+  const float *part = bias ? a.part_bias : a.part;
+  const int64_t i = ((int64_t)(bias ? blockIdx.x - a.weight_groups : blockIdx.x) * 16 + x) * 4;
+  F4 t = F4{};
+  if (i < n)
+    for (int p = y; p < a.slices; p += 16) t += *reinterpret_cast<const F4 *>(part + p * n + i);
+  s[y][x] = t;
+  __syncthreads();
+  if (y || i >= n) return;
+  t = F4{};
+#pragma unroll
+  for (int p = 0; p < 16; p++) t += s[p][x];
+  if (bias) {
+    for (int e = 0; e < 4; e++)
+      if (i + e < a.out) store_any(a.dbias, i + e, a.type, t[e]);
+    return;
+  }
+  const int per = a.kt * a.nt * 1024, tile = (int)(i / per), f = (int)(i - (int64_t)tile * per), frag = f / 1024, e = f / 256 % 4, lane = f / 4 % 64;
+  const int tk = tile / a.tiles_n, tn = tile - tk * a.tiles_n, fk = frag / a.nt, fn = frag - fk * a.nt;
+  const int k = (tk * a.kt + fk) * 32 + lane % 32, c = (tn * a.nt + fn) * 32 + 8 * e + 4 * (lane / 32);
+  if (k >= a.cols) return;
+  for (int j = 0; j < 4; j++)
+    if (c + j < a.out) store_any(a.dweight, (int64_t)k * a.ld_dw + c + j, a.type, t[j]);
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -818,26 +976,42 @@ template <class T, class TI, class TO, bool GRAD> static void linear_run(const L
   run(ntw == 1 ? k_linear_tile<T, TI, TO, 1, GRAD> : k_linear_tile<T, TI, TO, 2, GRAD>, grid, dim3(256), a);
 }
 
-struct GradPlan { int kt, nt, slices; int64_t slice; };
+// How the gradient's sums are cut: tiles of 32 kt columns by 32 nt of dz, and slices of the rows, two workgroups a CU.
+struct GradPlan { int kt, nt, tiles_k, tiles_n, slices; int64_t slice, part, part_bias; bool whole; };
 static GradPlan grad_plan(int64_t rows, int cols, int out) {
-  GradPlan p;
-  p.kt = cols > 64 ? 4 : 2;
-  p.nt = out > 64 ? 4 : 2;
-  const int64_t tiles = (int64_t)((cols + p.kt * 32 - 1) / (p.kt * 32)) * ((out + p.nt * 32 - 1) / (p.nt * 32));
-  const int64_t blocks = (rows + kGradRows - 1) / kGradRows;
-  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(blocks, 512 / tiles));
+  GradPlan p{};
+  const int k = (cols + 31) / 32, n = (out + 31) / 32;
+  p.kt = k <= 2 ? 2 : k <= 4 || n > 2 ? 4 : 8;
+  p.nt = n <= 2 ? 2 : n <= 4 || p.kt > 4 ? 4 : n <= 6 ? 6 : 4;
+  if (p.kt == 8) p.nt = 2;
+  p.tiles_k = (k + p.kt - 1) / p.kt;
+  p.tiles_n = (n + p.nt - 1) / p.nt;
+  p.whole = p.tiles_k == 1 && p.tiles_n == 1;
+  const int64_t blocks = (rows + kGradRows - 1) / kGradRows, tiles = (int64_t)p.tiles_k * p.tiles_n;
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>((blocks + 1) / 2, 512 / tiles));
   p.slice = (blocks + slices - 1) / slices * kGradRows;
   p.slices = (int)((rows + p.slice - 1) / p.slice);
+  p.part = p.slices * tiles * p.kt * p.nt * 1024;
+  p.part_bias = (int64_t)p.slices * p.tiles_n * p.nt * 32;
   return p;
 }
 
-template <class T, class TI> static void weight_grad_run(const WeightGradArgs &a, const GradPlan &p, Launches &run) {
-  const dim3 grid((a.cols + p.kt * 32 - 1) / (p.kt * 32), (a.out + p.nt * 32 - 1) / (p.nt * 32), p.slices), block(kLinearThreads);
-  if (a.part) {
-    if (p.kt == 2) run(p.nt == 2 ? k_weight_grad<T, TI, 2, 2> : k_weight_grad<T, TI, 2, 4>, grid, block, a);
-    else run(p.nt == 2 ? k_weight_grad<T, TI, 4, 2> : k_weight_grad<T, TI, 4, 4>, grid, block, a);
+template <class T, class TI, int KT, int NT> static void grad_launch(const GradArgs &a, const GradPlan &p, Launches &run) {
+  const dim3 grid(p.tiles_k, p.tiles_n, p.slices);
+  if constexpr (sizeof(T) == sizeof(TI) && (sizeof(T) == 2 || NT <= 4))
+    if (a.dx) return run(k_linear_grad<T, TI, KT, NT, true>, grid, dim3(kGradThreads), a);
+  run(k_linear_grad<T, TI, KT, NT, false>, grid, dim3(kGradThreads), a);
+}
+template <class T, class TI> static void grad_run(const GradArgs &a, const GradPlan &p, Launches &run) {
+  if (p.kt == 8) return grad_launch<T, TI, 8, 2>(a, p, run);
+  if (p.kt == 2) {
+    if (p.nt == 2) return grad_launch<T, TI, 2, 2>(a, p, run);
+    if (p.nt == 4) return grad_launch<T, TI, 2, 4>(a, p, run);
+    return grad_launch<T, TI, 2, 6>(a, p, run);
   }
-  if (a.part_bias) run(k_bias_grad<TI>, dim3((a.out + kWave - 1) / kWave, p.slices), dim3(kHeadThreads), a);
+  if (p.nt == 2) return grad_launch<T, TI, 4, 2>(a, p, run);
+  if (p.nt == 4) return grad_launch<T, TI, 4, 4>(a, p, run);
+  grad_launch<T, TI, 4, 6>(a, p, run);
 }
 
 static const char *linear_check(int64_t rows, int32_t cols, int32_t out, int32_t type, int32_t io_type, int32_t act) {
@@ -878,7 +1052,8 @@ extern "C" ink_status ink_linear(const void *x, int64_t ld_x, const void *weight
 
 extern "C" size_t ink_linear_backward_work(int64_t rows, int32_t cols, int32_t out) {
   if (rows < 1 || rows > kMaxHeadRows || cols < 1 || cols > INK_MAX_IN_DIM || out < 1 || out > INK_MAX_IN_DIM) return 0;
-  return (size_t)grad_plan(rows, cols, out).slices * ((size_t)cols + 1) * (size_t)out * sizeof(float);
+  const GradPlan p = grad_plan(rows, cols, out);
+  return (size_t)(p.part + p.part_bias) * sizeof(float);
 }
 
 extern "C" ink_status ink_linear_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const void *weight, int64_t ld_w,
@@ -900,33 +1075,41 @@ extern "C" ink_status ink_linear_backward(const void *dy, int64_t ld_dy, const v
   if (rows > 0 && (dweight || dbias) && (!work || !aligned_to(work, 16) || work_bytes < ink_linear_backward_work(rows, cols, out)))
     return fail_call(INK_E_ARG, "%s: work holds less than ink_linear_backward_work bytes or is not aligned to 16", who);
   Launches run(hip_stream);
-  if (dx && rows > 0) {
+  GradPlan p{};
+  if (rows > 0) p = grad_plan(rows, cols, out);
+  // dx in the same pass where one workgroup has all columns of both matrices and, in 32 bits, the registers for it
+  const bool sums = dweight || dbias, together = dx && sums && rows > 0 && p.whole && type == dy_type && (type != INK_F32 || p.nt <= 4);
+  if (act == INK_ACT_NONE) pre = nullptr;
+  if (dx && rows > 0 && !together) {
     LinearArgs a{};
-    a.in = dy; a.pre = act == INK_ACT_NONE ? nullptr : pre; a.weight = weight; a.out = dx;
+    a.in = dy; a.pre = pre; a.weight = weight; a.out = dx;
     a.rows = rows; a.ld_in = ld_dy; a.ld_pre = ld_pre; a.ld_w = ld_w; a.ld_out = ld_dx;
     a.depth = out; a.width = cols; a.act = act;
     if (type == INK_F32) linear_run<float, float, float, true>(a, run);
     else if (type == INK_F16) linear_run<f16, f16, f16, true>(a, run);
     else dy_type == INK_F32 ? linear_run<bf16, float, bf16, true>(a, run) : linear_run<bf16, bf16, bf16, true>(a, run);
   }
-  if (dweight || dbias) {
-    GradPlan p{};
-    WeightGradArgs a{};
+  if (sums) {
+    GradSumArgs s{};
+    s.type = type; s.cols = cols; s.out = out; s.dweight = dweight; s.dbias = dbias; s.ld_dw = ld_dw;
+    s.kt = s.nt = 2; s.tiles_k = (cols + 63) / 64; s.tiles_n = (out + 63) / 64;        // no rows: zeros
     if (rows > 0) {
-      p = grad_plan(rows, cols, out);
-      a.x = x; a.dy = dy; a.pre = act == INK_ACT_NONE ? nullptr : pre;
-      a.part = static_cast<float *>(work);
-      a.part_bias = dbias ? a.part + (int64_t)p.slices * cols * out : nullptr;
-      if (!dweight) a.part = nullptr;
-      a.rows = rows; a.ld_x = ld_x; a.ld_dy = ld_dy; a.ld_pre = ld_pre; a.slice = p.slice;
+      GradArgs a{};
+      a.x = x; a.dy = dy; a.pre = pre; a.weight = weight; a.dx = together ? dx : nullptr;
+      a.part = dweight ? static_cast<float *>(work) : nullptr;
+      a.part_bias = dbias ? static_cast<float *>(work) + p.part : nullptr;
+      a.rows = rows; a.ld_x = ld_x; a.ld_dy = ld_dy; a.ld_pre = ld_pre; a.ld_w = ld_w; a.ld_dx = ld_dx; a.slice = p.slice;
       a.cols = cols; a.out = out; a.act = act;
-      if (type == INK_F32) weight_grad_run<float, float>(a, p, run);
-      else if (type == INK_F16) weight_grad_run<f16, f16>(a, p, run);
-      else dy_type == INK_F32 ? weight_grad_run<bf16, float>(a, p, run) : weight_grad_run<bf16, bf16>(a, p, run);
+      if (!dweight) a.x = nullptr;           // not read
+      if (type == INK_F32) grad_run<float, float>(a, p, run);
+      else if (type == INK_F16) grad_run<f16, f16>(a, p, run);
+      else dy_type == INK_F32 ? grad_run<bf16, float>(a, p, run) : grad_run<bf16, bf16>(a, p, run);
+      s.part = a.part; s.part_bias = a.part_bias; s.slices = p.slices;
+      s.kt = p.kt; s.nt = p.nt; s.tiles_k = p.tiles_k; s.tiles_n = p.tiles_n;
     }
-    const int64_t n = (int64_t)cols * out;  // no rows: zeros
-    if (dweight) run(k_weight_sum, dim3((unsigned)((n + kHeadThreads - 1) / kHeadThreads)), dim3(kHeadThreads), a.part, n, p.slices, type, out, dweight, ld_dw);
-    if (dbias) run(k_weight_sum, dim3((out + kHeadThreads - 1) / kHeadThreads), dim3(kHeadThreads), a.part_bias, (int64_t)out, p.slices, type, out, dbias, (int64_t)out);
+    s.weight_groups = dweight ? s.tiles_k * s.tiles_n * s.kt * s.nt * 16 : 0;
+    const int bias_groups = dbias ? (s.tiles_n * s.nt + 1) / 2 : 0;
+    run(k_grad_sum, dim3(s.weight_groups + bias_groups), dim3(256), s);
   }
   return run.done(who);
 }
