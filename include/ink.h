@@ -52,7 +52,7 @@ extern "C" {
 #define INK_MAX_OUT_DIM 256
 #define INK_MAX_IN_DIM 16384
 #define INK_MAX_LAYERS 8
-#define INK_MAX_CLASSES (1 << 30) /* ink_log_probs: classes of a row, and alternatives asked for */
+#define INK_MAX_CLASSES (1 << 27) /* ink_log_probs: classes of a row, and alternatives asked for */
 #define INK_MAX_TOP 16
 
 typedef struct ink_ctx ink_ctx; /* opaque; owns all device state */

@@ -11,8 +11,13 @@
 // Bound by memory: a row is read once.  Short rows (k_probs_rows): L lanes hold a row in registers, in at most 4 loads a lane; the
 // maximum comes first and the sums after it, from the registers.  Long rows (k_probs_long): a workgroup, or several for parts
 // of a row where there are few rows, runs over the row with a running maximum that the sums follow; k_probs_join
-// puts the parts together.  The alternatives are kept as a sorted list a lane: an element goes through the list by
-// one comparison a place, and at the end the group takes the best head of all lists, once per alternative.
+// puts the parts together.
+//
+// The alternatives are what costs instructions.  They are kept as a sorted list a lane, and at the end the group takes the best head
+// of all lists, once per alternative.  An element is one number, its order above its class, so that a place of the list costs one
+// instruction (the median of the place, the one above and the element).  16-bit logits and their classes fit into 32 bits; of 32-bit logits
+// the lowest bits give way to the class, and where that leaves the order open (equal upper bits at the list's end or within it), or a row
+// has NaN, the row is done again by full comparisons.  In long rows a wave skips what is below K values it has seen.
 #include <algorithm>
 
 #include "head.h"
@@ -30,7 +35,7 @@ struct ProbsArgs {
   uint32_t *part_ord;                       // [rows][parts][top]
   int32_t *part_id;
   int64_t rows, ld, classes, part_len;
-  int parts, top, wide_targets;
+  int parts, top, wide_targets, id_bits;    // id_bits: of a number in a list that stand for the class (32-bit logits)
   float scale;
 };
 
@@ -49,10 +54,7 @@ __device__ __forceinline__ float of_order(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);      // all ones: a NaN
 }
 
-// A list of the K best elements of a lane, best first.
-//   f32            order and class apart
-//   bf16 and f16   one number: the 16 bits of the order above 65535 - index, the index being the class (short rows) or the place
-//                  among the lane's elements (long rows), so that a place of the list costs two instructions instead of five
+// A list of the K best elements of a lane, best first, order and class apart: five instructions a place.
 template <class T, int K> struct Best {
   uint32_t o[K > 0 ? K : 1];
   int32_t id[K > 0 ? K : 1];
@@ -77,18 +79,24 @@ template <class T, int K> struct Best {
   }
 };
 
-// The 16 bits of a bf16 or f16 in the same order.
-template <class T> __device__ __forceinline__ uint32_t order16(T v) {
-  const uint32_t u = __builtin_bit_cast(uint16_t, v);
-  constexpr uint32_t inf = __is_same(T, bf16) ? 0x7f80u : 0x7c00u;
-  uint32_t o = u & 0x8000u ? u ^ 0xffffu : u | 0x8000u;
-  o = u == 0x8000u ? 0x8000u : o;
-  return (u & 0x7fffu) > inf ? 0xffffu : o;
+// the place of x in a sorted list of numbers, best first: the median of three neighbours, from the end on
+__device__ __forceinline__ uint32_t median(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("v_med3_u32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
-template <class T> __device__ __forceinline__ float of_order16(uint32_t o) {
-  const uint16_t u = (uint16_t)(o & 0x8000u ? o ^ 0x8000u : o ^ 0xffffu);
-  return (float)__builtin_bit_cast(T, u);
+template <int K> __device__ __forceinline__ void put_number(uint32_t (&list)[K], uint32_t x) {
+#pragma unroll
+  for (int k = K - 1; k > 0; k--) list[k] = median(list[k - 1], list[k], x);
+  list[0] = max(list[0], x);
 }
+// order_of without the care for NaN
+__device__ __forceinline__ uint32_t order_of_number(float v) {
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+// bits of a number that stand for the class: what the order of a type leaves
+template <class T> constexpr int kIdBits = __is_same(T, bf16) ? 16 : 13;
 
 // Best of a group's heads, taken off its list: every lane gets it.
 template <int L, int K> __device__ __forceinline__ void take_best(Best<float, K> &b, uint32_t &o, int32_t &id) {
@@ -134,43 +142,32 @@ __device__ __forceinline__ void write_top(const ProbsArgs &a, int64_t r, int j, 
 template <class T, int L, int NV, int V, int K>
 __global__ __launch_bounds__(kHeadThreads) void k_probs_rows(ProbsArgs a) {
   constexpr int G = kHeadThreads / L;
-  constexpr bool PACKED = sizeof(T) == 2;
+  constexpr bool EXACT = sizeof(T) == 2;     // a number holds order and class
+  constexpr int KL = EXACT ? K : K + 1;      // ... or one more place says whether the last one is certain
   const int q = threadIdx.x % L, C = (int)a.classes;
+  const uint32_t low = (1u << (EXACT ? kIdBits<T> : a.id_bits)) - 1;
   for (int64_t r0 = (int64_t)blockIdx.x * G; r0 < a.rows; r0 += (int64_t)gridDim.x * G) {
     const int64_t mine = r0 + threadIdx.x / L;
     const int64_t r = mine < a.rows ? mine : a.rows - 1;
     const T *x = static_cast<const T *>(a.logits) + r * a.ld;
-    typename Pack<T, V>::type raw[NV];
+    float f[NV][V];
 #pragma unroll
-    for (int i = 0; i < NV; i++) raw[i] = *reinterpret_cast<const typename Pack<T, V>::type *>(x + min((i * L + q) * V, C - V));
+    for (int i = 0; i < NV; i++) load_pack<T, V>(x + min((i * L + q) * V, C - V), f[i]);
     const int64_t t = target_of(a.targets, a.wide_targets, r);
     const bool has = t >= 0 && t < C;
     const float zt = has ? (float)x[t] * a.scale : 0.f;
-    float z[NV][V];
-    float m = -__builtin_inff();
-    Best<T, PACKED ? 0 : K> best;                          // f32
-    uint32_t packed[PACKED && K > 0 ? K : 1];
-    best.clear();
-    if constexpr (PACKED)
+    uint32_t list[KL > 0 ? KL : 1];
 #pragma unroll
-      for (int k = 0; k < K; k++) packed[k] = 0;
+    for (int k = 0; k < KL; k++) list[k] = 0;
+    float m = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       const int first = (i * L + q) * V, at = min(first, C - V);
 #pragma unroll
       for (int j = 0; j < V; j++) {
-        T e;
-        if constexpr (V == 1) e = raw[i]; else e = raw[i][j];
         const bool live = at + j >= first;                 // the rest is a repetition of the vector before
-        z[i][j] = live ? (float)e * a.scale : -__builtin_inff();
-        m = fmaxf(m, z[i][j]);
-        if constexpr (K > 0) {
-          if constexpr (PACKED) {
-            uint32_t key = live ? order16<T>(e) << 16 | (uint32_t)(0xffff - (at + j)) : 0u;
-#pragma unroll
-            for (int k = 0; k < K; k++) { const uint32_t hi = max(packed[k], key); key = min(packed[k], key); packed[k] = hi; }
-          } else best.put(live ? order_of((float)e) : 0u, at + j);
-        }
+        m = fmaxf(m, live ? f[i][j] * a.scale : -__builtin_inff());
+        if constexpr (K > 0) put_number<KL>(list, live ? (order_of_number(f[i][j]) & ~low) | (low - (uint32_t)(at + j)) : 0u);
       }
     }
     m = group_all<L>(m, [](float p, float p2) { return fmaxf(p, p2); });
@@ -179,7 +176,10 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_rows(ProbsArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; i++)
 #pragma unroll
-      for (int j = 0; j < V; j++) add_term(z[i][j], ms, s, u);
+      for (int j = 0; j < V; j++) {
+        const int first = (i * L + q) * V, at = min(first, C - V);
+        add_term(at + j >= first ? f[i][j] * a.scale : -__builtin_inff(), ms, s, u);
+      }
     s = group_sum<L>(s);
     u = group_sum<L>(u);
     const bool on = mine < a.rows;
@@ -187,23 +187,46 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_rows(ProbsArgs a) {
     if (on && q == 0) lse = finish_row(a, r, ms, s, u, zt, has);
     else lse = s == 0.f ? -__builtin_inff() : ms + logf(s);
     if constexpr (K > 0) {
+      uint32_t o[KL];
+      bool open = s != s;                    // a NaN (or +inf) in the row
 #pragma unroll
-      for (int k = 0; k < K; k++) {
-        uint32_t o; int32_t id; float v;
-        if constexpr (PACKED) {
-          o = group_all<L>(packed[0], [](uint32_t p, uint32_t p2) { return p > p2 ? p : p2; });
-          const bool me = packed[0] == o;
+      for (int k = 0; k < KL; k++) {
+        o[k] = group_all<L>(list[0], [](uint32_t p, uint32_t p2) { return p > p2 ? p : p2; });
+        const bool me = list[0] == o[k];
 #pragma unroll
-          for (int i = 0; i + 1 < K; i++) packed[i] = me ? packed[i + 1] : packed[i];
-          packed[K - 1] = me ? 0 : packed[K - 1];
-          id = 0xffff - (int32_t)(o & 0xffffu);
-          v = of_order16<T>(o >> 16);
-        } else {
-          take_best<L, K>(best, o, id);
-          v = of_order(o);
-        }
-        if (on && q == k % L && k < a.top) write_top(a, r, k, v, id, lse);
+        for (int i = 0; i + 1 < KL; i++) list[i] = me ? list[i + 1] : list[i];
+        list[KL - 1] = me ? 0 : list[KL - 1];
+        if constexpr (!EXACT)
+          if (k > 0) open |= k <= a.top && o[k] != 0 && ((o[k] ^ o[k - 1]) & ~low) == 0;
       }
+      int32_t id[K > L ? (K + L - 1) / L : 1];               // this lane's alternatives: q, q + L, ...
+      float v[K > L ? (K + L - 1) / L : 1];
+      if (!__any(open)) {
+#pragma unroll
+        for (int i = 0; i * L < K; i++) {
+          uint32_t mine_o = o[i * L];
+#pragma unroll
+          for (int k = 1; k < L; k++)
+            if (i * L + k < K) mine_o = q == k ? o[i * L + k] : mine_o;
+          id[i] = (int32_t)(low - (mine_o & low));
+          if constexpr (EXACT) v[i] = of_order(mine_o & 0x80000000u ? mine_o & ~low : mine_o | low);
+          else v[i] = on && i * L + q < a.top ? (float)x[id[i]] : 0.f;
+        }
+      } else {                               // once more from memory: rare, and not to cost the usual case registers
+        Best<float, K> best;
+        best.clear();
+#pragma unroll 1
+        for (int c = q; c < C; c += L) best.put(order_of((float)x[c]), c);
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+          uint32_t oo; int32_t ii;
+          take_best<L, K>(best, oo, ii);
+          if (q == k % L) { id[k / L] = ii; v[k / L] = of_order(oo); }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i * L < K; i++)
+        if (on && i * L + q < a.top) write_top(a, r, i * L + q, v[i], id[i], lse);
     }
   }
 }
@@ -237,153 +260,178 @@ template <int K> __device__ __forceinline__ void block_best(Best<float, K> &b, u
   __syncthreads();
 }
 
-template <class T, int V, int K>
+// TW: threads of a row (or part): a workgroup, or one wave where there are rows for all of them, which then needs no LDS at the end.
+template <class T, int V, int K, int TW>
 __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
-  constexpr int W = kHeadThreads / kWave, KS = K > 0 ? K : 1;
-  constexpr bool PACKED = sizeof(T) == 2;
+  constexpr int W = kHeadThreads / kWave, G = kHeadThreads / TW, KS = K > 0 ? K : 1;
+  // 16-bit logits: a number is the order above the place among the lane's elements, of which probs_parts leaves few enough
+  constexpr bool EXACT = sizeof(T) == 2;
+  constexpr uint32_t low = (1u << kIdBits<T>) - 1;
   __shared__ float s_m[W], s_s[W], s_u[W];
   __shared__ uint32_t s_o[(W + 1) * KS];
   __shared__ int32_t s_id[(W + 1) * KS];
-  const int64_t r = blockIdx.x / (unsigned)a.parts;
-  const int part = (int)(blockIdx.x % (unsigned)a.parts);
-  const int64_t c0 = part * a.part_len, c1 = min(c0 + a.part_len, a.classes);    // part_len is a multiple of V
-  const T *x = static_cast<const T *>(a.logits) + r * a.ld;
-  RowStats st = {-__builtin_inff(), 0.f, 0.f};
-  Best<float, K> best;
-  best.clear();
-  uint32_t packed[KS];
+  const int tid = threadIdx.x % TW;
+  for (int64_t item = (int64_t)blockIdx.x * G + threadIdx.x / TW; item < a.rows * a.parts; item += (int64_t)gridDim.x * G) {
+    auto order_of_list = [](uint32_t number) { return number == 0 ? 0u : number & 0x80000000u ? number & ~low : number | low; };
+    const int64_t r = item / a.parts;
+    const int part = (int)(item - r * a.parts);
+    const int64_t c0 = part * a.part_len, c1 = min(c0 + a.part_len, a.classes);    // part_len is a multiple of V
+    const T *x = static_cast<const T *>(a.logits) + r * a.ld;
+    RowStats st = {-__builtin_inff(), 0.f, 0.f};
+    Best<float, K> best;
+    best.clear();
+    uint32_t list[KS];
 #pragma unroll
-  for (int k = 0; k < KS; k++) packed[k] = 0;
-  uint32_t floor_o = 0;                    // K elements of the wave are at least this large
-  int64_t refresh = 1;
-  int step = 0;
-  const int64_t n_vec = (c1 - c0 + V - 1) / V;
-  for (int64_t i0 = 0; i0 < n_vec; i0 += kHeadThreads, step++) {
-    const int64_t i = i0 + threadIdx.x;
-    const int64_t first = c0 + i * V;
-    const int64_t at = min(first, a.classes - V);
-    const typename Pack<T, V>::type raw = *reinterpret_cast<const typename Pack<T, V>::type *>(x + at);
-    float z[V];
-    uint32_t o[V];
-    float vm = -__builtin_inff();
-    uint32_t vo = 0;
+    for (int k = 0; k < KS; k++) list[k] = 0;
+    float floor_z = -__builtin_inff();       // K elements of the wave are at least this large
+    int64_t refresh = 1, step = 0;
+    const int64_t n_vec = (c1 - c0 + V - 1) / V;
+    for (int64_t i0 = 0; i0 < n_vec; i0 += TW, step++) {
+      const int64_t first = c0 + (i0 + tid) * V, at = min(first, a.classes - V);
+      float f[V], z[V];
+      load_pack<T, V>(x + at, f);
+      float vm = -__builtin_inff();
 #pragma unroll
-    for (int j = 0; j < V; j++) {
-      const bool live = at + j >= first && first < c1;
-      z[j] = live ? (float)raw[j] * a.scale : -__builtin_inff();
-      vm = fmaxf(vm, z[j]);
-      if constexpr (K > 0) {
-        if constexpr (PACKED) o[j] = live ? order16<T>(raw[j]) : 0u;
-        else o[j] = live ? order_of((float)raw[j]) : 0u;
-        vo = max(vo, o[j]);
+      for (int j = 0; j < V; j++) {
+        z[j] = at + j >= first && first < c1 ? f[j] * a.scale : -__builtin_inff();
+        vm = fmaxf(vm, z[j]);
       }
-    }
-    if (vm > st.m) rescale(st, vm);
-    const float ms = safe_max(st.m);
+      if (vm > st.m) rescale(st, vm);
+      const float ms = safe_max(st.m);
 #pragma unroll
-    for (int j = 0; j < V; j++) add_term(z[j], ms, st.s, st.u);
-    if constexpr (K > 0) {
-      const uint32_t last = PACKED ? packed[KS - 1] >> 16 : best.o[KS - 1];
-      if (__any(vo > last && vo >= floor_o)) {
+      for (int j = 0; j < V; j++) add_term(z[j], ms, st.s, st.u);
+      if constexpr (K > 0) {
+        if (__any(vm >= floor_z)) {
 #pragma unroll
-        for (int j = 0; j < V; j++) {
-          if (!__any(o[j] > (PACKED ? packed[KS - 1] >> 16 : best.o[KS - 1]) && o[j] >= floor_o)) continue;
-          if constexpr (PACKED) {
-            uint32_t key = o[j] ? o[j] << 16 | (uint32_t)(0xffff - (step * V + j)) : 0u;
+          for (int j = 0; j < V; j++) {
+            const bool live = at + j >= first && first < c1;
+            const uint32_t o = live && z[j] >= floor_z ? order_of_number(f[j]) : 0u;
+            if constexpr (EXACT) {
+              const uint32_t number = o ? (o & ~low) | (low - (uint32_t)(step * V + j)) : 0u;
+              if (__any(number > list[KS - 1])) put_number<KS>(list, number);
+            } else if (__any(o > best.o[KS - 1])) best.put(o, (int32_t)(at + j));
+          }
+        }
+        if (step + 1 == refresh) {           // at steps 1, 2, 4, ...: the K-th best of the lanes' best
+          refresh *= 2;
+          uint32_t head = EXACT ? order_of_list(list[0]) : best.o[0], o = 0;
 #pragma unroll
-            for (int k = 0; k < K; k++) { const uint32_t hi = max(packed[k], key); key = min(packed[k], key); packed[k] = hi; }
-          } else best.put(o[j], (int32_t)(at + j));
+          for (int k = 0; k < K; k++) {
+            o = group_all<kWave>(head, [](uint32_t p, uint32_t p2) { return p > p2 ? p : p2; });
+            const uint64_t who = __ballot(head == o);
+            head = lane_id() == __ffsll((unsigned long long)who) - 1 ? 0u : head;
+          }
+          if (o) floor_z = of_order(o) * a.scale;
         }
       }
-      if (step + 1 == refresh) {           // at steps 1, 2, 4, ...: the K-th best of the lanes' best
-        refresh *= 2;
-        uint32_t head = PACKED ? packed[0] >> 16 : best.o[0];
+    }
+    // the row's sums
+    float bm = group_all<kWave>(st.m, [](float p, float p2) { return fmaxf(p, p2); });
+    if constexpr (TW > kWave) {
+      if (lane_id() == 0) s_m[threadIdx.x / kWave] = bm;
+      __syncthreads();
+      bm = s_m[0];
+#pragma unroll
+      for (int w = 1; w < W; w++) bm = fmaxf(bm, s_m[w]);
+    }
+    rescale(st, safe_max(bm));
+    float s = group_sum<kWave>(st.s), u = group_sum<kWave>(st.u);
+    if constexpr (TW > kWave) {
+      if (lane_id() == 0) { s_s[threadIdx.x / kWave] = s; s_u[threadIdx.x / kWave] = u; }
+      __syncthreads();
+      s = u = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; w++) { s += s_s[w]; u += s_u[w]; }
+    }
+    if constexpr (K > 0) {
+      if constexpr (EXACT)                   // from places to classes
 #pragma unroll
         for (int k = 0; k < K; k++) {
-          floor_o = group_all<kWave>(head, [](uint32_t p, uint32_t p2) { return p > p2 ? p : p2; });
-          const uint64_t who = __ballot(head == floor_o);
-          head = lane_id() == __ffsll((unsigned long long)who) - 1 ? 0u : head;
+          const int64_t e = low - (list[k] & low), first = c0 + (e / V * TW + tid) * V;
+          best.o[k] = list[k] ? order_of_list(list[k]) : 0u;
+          best.id[k] = list[k] ? (int32_t)(min(first, a.classes - V) + e % V) : 0x7fffffff;
+        }
+      if (s != s) {                          // a NaN (or +inf) in the part: comparisons skipped it
+        best.clear();
+        for (int64_t i = tid; i < n_vec; i += TW) {
+          const int64_t first = c0 + i * V, at = min(first, a.classes - V);
+          float f[V];
+          load_pack<T, V>(x + at, f);
+#pragma unroll
+          for (int j = 0; j < V; j++) best.put(at + j >= first ? order_of(f[j]) : 0u, (int32_t)(at + j));
         }
       }
+      if constexpr (TW > kWave) block_best<K>(best, s_o, s_id);
     }
-  }
-  // the workgroup's sums
-  const float m = group_all<kWave>(st.m, [](float p, float p2) { return fmaxf(p, p2); });
-  if (lane_id() == 0) s_m[threadIdx.x / kWave] = m;
-  __syncthreads();
-  float bm = s_m[0];
-#pragma unroll
-  for (int w = 1; w < W; w++) bm = fmaxf(bm, s_m[w]);
-  rescale(st, safe_max(bm));
-  st.s = group_sum<kWave>(st.s);
-  st.u = group_sum<kWave>(st.u);
-  if (lane_id() == 0) { s_s[threadIdx.x / kWave] = st.s; s_u[threadIdx.x / kWave] = st.u; }
-  if constexpr (K > 0) {
-    if constexpr (PACKED)                  // from places among the lane's elements to classes
-#pragma unroll
-      for (int k = 0; k < K; k++) {
-        const int e = 0xffff - (int)(packed[k] & 0xffffu);
-        const int64_t first = c0 + ((int64_t)(e / V) * kHeadThreads + threadIdx.x) * V;
-        best.o[k] = packed[k] ? order_of(of_order16<T>(packed[k] >> 16)) : 0u;
-        best.id[k] = packed[k] ? (int32_t)(min(first, a.classes - V) + e % V) : 0x7fffffff;
-      }
-    block_best<K>(best, s_o, s_id);
-  } else __syncthreads();
-  float s = 0.f, u = 0.f;
-#pragma unroll
-  for (int w = 0; w < W; w++) { s += s_s[w]; u += s_u[w]; }
-  if (a.parts > 1) {
     const int64_t p = r * a.parts + part;
-    if (threadIdx.x == 0) { a.part_stats[3 * p] = bm; a.part_stats[3 * p + 1] = s; a.part_stats[3 * p + 2] = u; }
-    if (K > 0 && (int)threadIdx.x < a.top) {
-      a.part_ord[p * a.top + threadIdx.x] = s_o[W * KS + threadIdx.x];
-      a.part_id[p * a.top + threadIdx.x] = s_id[W * KS + threadIdx.x];
+    if (a.parts > 1) {
+      if (threadIdx.x == 0) { a.part_stats[3 * p] = bm; a.part_stats[3 * p + 1] = s; a.part_stats[3 * p + 2] = u; }
+      if (K > 0 && (int)threadIdx.x < a.top) {
+        a.part_ord[p * a.top + threadIdx.x] = s_o[W * KS + threadIdx.x];
+        a.part_id[p * a.top + threadIdx.x] = s_id[W * KS + threadIdx.x];
+      }
+    } else {
+      const float ms = safe_max(bm);
+      const float lse = s == 0.f ? -__builtin_inff() : ms + logf(s);
+      if (tid == 0) {
+        const int64_t t = target_of(a.targets, a.wide_targets, r);
+        const bool has = t >= 0 && t < a.classes;
+        finish_row(a, r, ms, s, u, has ? (float)x[t] * a.scale : 0.f, has);
+      }
+      if constexpr (K > 0) {
+        uint32_t o = 0;
+        int32_t id = 0;
+        if constexpr (TW > kWave) {
+          if (tid < K) { o = s_o[W * KS + tid]; id = s_id[W * KS + tid]; }
+        } else {
+#pragma unroll
+          for (int k = 0; k < K; k++) {
+            uint32_t oo; int32_t ii;
+            take_best<kWave, K>(best, oo, ii);
+            if (tid == k) { o = oo; id = ii; }
+          }
+        }
+        if (tid < a.top) write_top(a, r, tid, of_order(o), id, lse);
+      }
     }
-    return;
+    if constexpr (TW > kWave) __syncthreads();               // LDS is the next row's
   }
-  const float ms = safe_max(bm);
-  const float lse = s == 0.f ? -__builtin_inff() : ms + logf(s);
-  if (threadIdx.x == 0) {
-    const int64_t t = target_of(a.targets, a.wide_targets, r);
-    const bool has = t >= 0 && t < a.classes;
-    finish_row(a, r, ms, s, u, has ? (float)x[t] * a.scale : 0.f, has);
-  }
-  if (K > 0 && (int)threadIdx.x < a.top) write_top(a, r, threadIdx.x, of_order(s_o[W * KS + threadIdx.x]), s_id[W * KS + threadIdx.x], lse);
 }
 
 // Parts of a row, at most 64, to the row: one wave a row, a part a lane.
 template <class T, int K>
 __global__ __launch_bounds__(kWave) void k_probs_join(ProbsArgs a) {
-  const int64_t r = blockIdx.x;
   const int l = lane_id();
-  const int64_t p = r * a.parts + min(l, a.parts - 1);
-  RowStats st = {a.part_stats[3 * p], a.part_stats[3 * p + 1], a.part_stats[3 * p + 2]};
-  if (l >= a.parts) st = {-__builtin_inff(), 0.f, 0.f};
-  const float m = safe_max(group_all<kWave>(st.m, [](float x, float y) { return fmaxf(x, y); }));
-  rescale(st, m);
-  const float s = group_sum<kWave>(st.s), u = group_sum<kWave>(st.u);
-  const float lse = s == 0.f ? -__builtin_inff() : m + logf(s);
-  if (l == 0) {
-    const T *x = static_cast<const T *>(a.logits) + r * a.ld;
-    const int64_t t = target_of(a.targets, a.wide_targets, r);
-    const bool has = t >= 0 && t < a.classes;
-    finish_row(a, r, m, s, u, has ? (float)x[t] * a.scale : 0.f, has);
-  }
-  if constexpr (K > 0) {
-    Best<float, K> b;
-    b.clear();
-    if (l < a.parts)
-#pragma unroll
-      for (int k = 0; k < K; k++)
-        if (k < a.top) { b.o[k] = a.part_ord[p * a.top + k]; b.id[k] = a.part_id[p * a.top + k]; }
-    uint32_t my_o = 0; int32_t my_id = 0;
-#pragma unroll
-    for (int k = 0; k < K; k++) {
-      uint32_t o; int32_t id;
-      take_best<kWave, K>(b, o, id);
-      if (l == k) { my_o = o; my_id = id; }
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const int64_t p = r * a.parts + min(l, a.parts - 1);
+    RowStats st = {a.part_stats[3 * p], a.part_stats[3 * p + 1], a.part_stats[3 * p + 2]};
+    if (l >= a.parts) st = {-__builtin_inff(), 0.f, 0.f};
+    const float m = safe_max(group_all<kWave>(st.m, [](float x, float y) { return fmaxf(x, y); }));
+    rescale(st, m);
+    const float s = group_sum<kWave>(st.s), u = group_sum<kWave>(st.u);
+    const float lse = s == 0.f ? -__builtin_inff() : m + logf(s);
+    if (l == 0) {
+      const T *x = static_cast<const T *>(a.logits) + r * a.ld;
+      const int64_t t = target_of(a.targets, a.wide_targets, r);
+      const bool has = t >= 0 && t < a.classes;
+      finish_row(a, r, m, s, u, has ? (float)x[t] * a.scale : 0.f, has);
     }
-    if (l < a.top) write_top(a, r, l, of_order(my_o), my_id, lse);
+    if constexpr (K > 0) {
+      Best<float, K> b;
+      b.clear();
+      if (l < a.parts)
+#pragma unroll
+        for (int k = 0; k < K; k++)
+          if (k < a.top) { b.o[k] = a.part_ord[p * a.top + k]; b.id[k] = a.part_id[p * a.top + k]; }
+      uint32_t my_o = 0; int32_t my_id = 0;
+#pragma unroll
+      for (int k = 0; k < K; k++) {
+        uint32_t o; int32_t id;
+        take_best<kWave, K>(b, o, id);
+        if (l == k) { my_o = o; my_id = id; }
+      }
+      if (l < a.top) write_top(a, r, l, of_order(my_o), my_id, lse);
+    }
   }
 }
 
@@ -432,6 +480,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_grad(ProbsGradArgs a) {
 }
 
 // ------------------------------------------------------------------------------------ host side
+constexpr int64_t kWaveRows = 4096;         // long rows of which a wave takes one: 16 waves a CU
 constexpr int kProbsVectors = 4;            // loads a lane, at most, of a short row
 static int probs_lanes(int64_t n_vec) {
   int l = 2;
@@ -446,8 +495,10 @@ static bool probs_long(int64_t classes, int type) {
 static int probs_parts(int64_t rows, int64_t classes, int type, int64_t *len) {
   const int64_t V = 16 / type_size(type), n_vec = (classes + V - 1) / V;
   int64_t parts = std::min<int64_t>({kWave, std::max<int64_t>(1, 1024 / rows), (n_vec + 4 * kHeadThreads - 1) / (4 * kHeadThreads)});
-  const int64_t most = (int64_t)65536 / V * kHeadThreads;  // places that 16 bits number (see Best)
-  const int64_t per = std::min((n_vec + parts - 1) / parts, most);
+  const int64_t most = (int64_t)8192 * kHeadThreads;       // elements of a part: a lane's places have 13 bits
+  static_assert(INK_MAX_CLASSES <= kWave * 8192ll * kHeadThreads, "64 parts are enough");
+  parts = std::max(parts, (n_vec * V + most - 1) / most);
+  const int64_t per = (n_vec + parts - 1) / parts;
   parts = (n_vec + per - 1) / per;
   *len = per * V;
   return (int)parts;
@@ -464,7 +515,9 @@ template <class T, int L, int K> static void probs_rows(const ProbsArgs &a, Laun
 template <class T, int K> static void probs_top(const ProbsArgs &a, Launches &run) {
   constexpr int V = 16 / sizeof(T);
   if (probs_long(a.classes, sizeof(T) == 4 ? INK_F32 : INK_BF16)) {
-    run(k_probs_long<T, V, K>, dim3((unsigned)(a.rows * a.parts)), dim3(kHeadThreads), a);
+    if (a.parts == 1 && a.rows >= kWaveRows && a.classes <= 8192 * kWave)
+      return run(k_probs_long<T, V, K, kWave>, dim3((unsigned)std::min<int64_t>((a.rows + 3) / 4, 1 << 20)), dim3(kHeadThreads), a);
+    run(k_probs_long<T, V, K, kHeadThreads>, dim3((unsigned)std::min<int64_t>(a.rows * a.parts, 1 << 20)), dim3(kHeadThreads), a);
     if (a.parts > 1) run(k_probs_join<T, K>, dim3((unsigned)a.rows), dim3(kWave), a);
     return;
   }
@@ -557,9 +610,9 @@ extern "C" ink_status ink_log_probs(const void *logits, int64_t ld, const void *
   a.logits = logits; a.targets = targets; a.wide_targets = target_bytes == 8;
   a.logp = logp; a.entropy = entropy; a.lse = lse; a.top_ids = top_ids; a.top_logp = top_logp;
   a.rows = rows; a.ld = ld; a.classes = classes; a.top = top; a.scale = scale; a.parts = 1;
+  while (a.id_bits < 16 && (1 << a.id_bits) < classes) a.id_bits++;
   if (probs_long(classes, type)) {
     a.parts = probs_parts(rows, classes, type, &a.part_len);
-    if (rows * a.parts > kMaxHeadRows) return fail_call(INK_E_RANGE, "%s: too many rows of so many classes", who);
     a.part_stats = static_cast<float *>(work);
     a.part_ord = reinterpret_cast<uint32_t *>(a.part_stats + 3 * rows * a.parts);
     a.part_id = reinterpret_cast<int32_t *>(a.part_ord + rows * a.parts * top);
