@@ -41,16 +41,12 @@ def _functions():
     return _fn
 
 
-def _check(lib, status):
-    if status != 0:
-        raise InkError(status, lib.ink_last_error(None).decode())
-
-
 def _matrix(t, name, rows=None, cols=None, dtype=None, like=None):
-    """t as a matrix of contiguous rows on a GPU; raises where it is none or not of this shape, type and device."""
+    """t as a matrix of contiguous rows on a GPU, and the distance of its rows; raises where it is none or not of this
+    shape, type and device."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
         raise ValueError("%s must be a 2-D GPU tensor" % name)
-    if t.dtype not in TYPES or (dtype is not None and t.dtype != dtype):
+    if t.dtype is not dtype and (dtype is not None or t.dtype not in TYPES):
         raise TypeError("%s has type %s, wanted %s" % (name, t.dtype, dtype or "float32, bfloat16 or float16"))
     n, m = t.shape
     if (rows is not None and n != rows) or (cols is not None and m != cols):
@@ -60,185 +56,184 @@ def _matrix(t, name, rows=None, cols=None, dtype=None, like=None):
     s0, s1 = t.stride()
     if (s1 != 1 and m > 1) or (s0 < m and s0 != 0 and n > 1):
         t = t.contiguous()
-    return t
+        s0 = m
+    return t, s0
 
 
 def _vector(t, name, n, like, dtypes):
+    """t as a contiguous vector of n elements, or None as it is."""
+    if t is None:
+        return None
     if not isinstance(t, torch.Tensor) or t.device != like.device or t.dim() != 1 or t.shape[0] != n:
         raise ValueError("%s must be a GPU tensor of shape [%d] on the rows' device" % (name, n))
     if t.dtype not in dtypes:
         raise TypeError("%s has type %s, wanted %s" % (name, t.dtype, " or ".join(str(d) for d in dtypes)))
-    return t if t.is_contiguous() else t.contiguous()
+    return t if n < 2 or t.stride(0) == 1 else t.contiguous()
+
+
+def _given(t, name):
+    """A tensor that this call cannot do without."""
+    if t is None:
+        raise ValueError("%s is missing" % name)
+    return t
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(t):
-    return torch.cuda.current_stream(t.device).cuda_stream
+def _call(fn, like, *args):
+    """fn(*args, stream) on the tensors' device; the raw-stream call is what torch's own stream objects are made from."""
+    dev, had = like.device.index, torch._C._cuda_getDevice()
+    if had == dev:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if status != 0:
+        raise InkError(status, _fn.ink_last_error(None).decode())
 
 
-class _on:
-    """Makes the tensors' device the current one for a call, where it is not."""
-
-    def __init__(self, t):
-        self.want = t.device.index
-
-    def __enter__(self):
-        self.had = torch.cuda.current_device()
-        if self.had != self.want:
-            torch.cuda.set_device(self.want)
-
-    def __exit__(self, *_):
-        if self.had != self.want:
-            torch.cuda.set_device(self.had)
+_F32 = (torch.float32,)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """(y, mean, rstd) of rows x: y = (x - mean) * rstd * weight + bias.  weight and bias: [cols] of x's type
     or float32 (both alike), or None; mean and rstd (float32) are what the gradient takes."""
-    x = _matrix(x, "x")
+    x, ld = _matrix(x, "x")
     rows, cols = x.shape
-    params = (x.dtype, torch.float32)
-    weight = None if weight is None else _vector(weight, "weight", cols, x, params)
-    bias = None if bias is None else _vector(bias, "bias", cols, x, params if weight is None else (weight.dtype,))
-    param = weight if weight is not None else bias
+    t = x.dtype
+    weight = _vector(weight, "weight", cols, x, (t, torch.float32))
+    param = t if weight is None else weight.dtype
+    bias = _vector(bias, "bias", cols, x, (t, torch.float32) if weight is None else (param,))
+    if weight is None and bias is not None:
+        param = bias.dtype
     lib = _functions()
-    y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    mean, rstd = (torch.empty(rows, dtype=torch.float32, device=x.device) for _ in range(2))
-    with _on(x):
-        _check(lib, lib.ink_layer_norm(x.data_ptr(), x.stride(0), _ptr(weight), _ptr(bias), rows, cols, TYPES[x.dtype],
-                                       TYPES[x.dtype if param is None else param.dtype], eps, y.data_ptr(), cols, mean.data_ptr(),
-                                       rstd.data_ptr(), _stream(x)))
+    y = x.new_empty((rows, cols))
+    mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
+    at = mean.data_ptr()
+    _call(lib.ink_layer_norm, x, x.data_ptr(), ld, _ptr(weight), _ptr(bias), rows, cols, TYPES[t], TYPES[param], eps, y.data_ptr(), cols, at,
+          at + 4 * rows)
     return y, mean, rstd
 
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, param_dtype=None, need_dx=True, need_params=True):
     """(dx, dweight, dbias) of layer_norm; None for what is not needed.  dweight and dbias have the weight's type,
     or param_dtype (x's type or float32) where there is no weight."""
-    x = _matrix(x, "x")
+    x, ld = _matrix(x, "x")
     rows, cols = x.shape
-    dy = _matrix(dy, "dy", rows, cols, x.dtype, x)
-    mean, rstd = (_vector(v, n, rows, x, (torch.float32,)) for v, n in ((mean, "mean"), (rstd, "rstd")))
+    t = x.dtype
+    dy, ld_dy = _matrix(dy, "dy", rows, cols, t, x)
+    mean, rstd = _vector(_given(mean, "mean"), "mean", rows, x, _F32), _vector(_given(rstd, "rstd"), "rstd", rows, x, _F32)
+    weight = _vector(weight, "weight", cols, x, (t, torch.float32))
     if weight is not None:
-        weight = _vector(weight, "weight", cols, x, (x.dtype, torch.float32))
         if param_dtype not in (None, weight.dtype):
             raise TypeError("param_dtype differs from the weight's type")
         param_dtype = weight.dtype
-    elif param_dtype not in (None, x.dtype, torch.float32):
+    elif param_dtype not in (None, t, torch.float32):
         raise TypeError("param_dtype must be x's type or float32")
-    param_dtype = param_dtype or x.dtype
+    param_dtype = param_dtype or t
     lib = _functions()
-    dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if need_dx else None
+    dx = x.new_empty((rows, cols)) if need_dx else None
     dweight = dbias = work = None
     n_work = 0
     if need_params:
-        dweight, dbias = (torch.empty(cols, dtype=param_dtype, device=x.device) for _ in range(2))
-        n_work = lib.ink_layer_norm_backward_work(rows, cols, TYPES[x.dtype])
-        work = torch.empty(n_work, dtype=torch.uint8, device=x.device)
-    with _on(x):
-        _check(lib, lib.ink_layer_norm_backward(dy.data_ptr(), dy.stride(0), x.data_ptr(), x.stride(0), mean.data_ptr(), rstd.data_ptr(),
-                                                _ptr(weight), rows, cols, TYPES[x.dtype], TYPES[param_dtype], _ptr(dx), cols,
-                                                _ptr(dweight), _ptr(dbias), _ptr(work), n_work, _stream(x)))
+        dweight, dbias = x.new_empty(cols, dtype=param_dtype), x.new_empty(cols, dtype=param_dtype)
+        n_work = lib.ink_layer_norm_backward_work(rows, cols, TYPES[t])
+        work = x.new_empty(n_work, dtype=torch.uint8) if n_work else None
+    _call(lib.ink_layer_norm_backward, x, dy.data_ptr(), ld_dy, x.data_ptr(), ld, mean.data_ptr(), rstd.data_ptr(), _ptr(weight), rows, cols,
+          TYPES[t], TYPES[param_dtype], _ptr(dx), cols, _ptr(dweight), _ptr(dbias), _ptr(work), n_work)
     return dx, dweight, dbias
 
 
 def linear(x, weight, bias=None, act="none", residual=None, keep_pre=False, out_dtype=None):
     """act(x @ weight + bias) + residual, with weight [cols, out]; (y, z) with keep_pre, z = x @ weight + bias being what the
     gradient of an activation takes.  act: none, relu, gelu, silu.  out_dtype (type of y, z and residual): x's or float32."""
-    x = _matrix(x, "x")
+    x, ld = _matrix(x, "x")
     rows, cols = x.shape
-    weight = _matrix(weight, "weight", cols, None, x.dtype, x)
+    t = x.dtype
+    weight, ld_w = _matrix(weight, "weight", cols, None, t, x)
     out = weight.shape[1]
-    bias = None if bias is None else _vector(bias, "bias", out, x, (x.dtype,))
-    out_dtype = out_dtype or x.dtype
-    if out_dtype not in (x.dtype, torch.float32):
+    bias = _vector(bias, "bias", out, x, (t,))
+    out_dtype = out_dtype or t
+    if out_dtype is not t and out_dtype is not torch.float32:
         raise TypeError("out_dtype must be x's type or float32")
     if act not in ACTS:
         raise ValueError("act must be one of %s" % ", ".join(ACTS))
-    residual = None if residual is None else _matrix(residual, "residual", rows, out, out_dtype, x)
+    ld_res = 0
+    if residual is not None:
+        residual, ld_res = _matrix(residual, "residual", rows, out, out_dtype, x)
     lib = _functions()
-    y = torch.empty((rows, out), dtype=out_dtype, device=x.device)
-    pre = torch.empty_like(y) if keep_pre else None
-    with _on(x):
-        _check(lib, lib.ink_linear(x.data_ptr(), x.stride(0), weight.data_ptr(), weight.stride(0), _ptr(bias), _ptr(residual),
-                                   0 if residual is None else residual.stride(0), rows, cols, out, TYPES[x.dtype], TYPES[out_dtype],
-                                   ACTS[act], y.data_ptr(), out, _ptr(pre), out, _stream(x)))
+    y = x.new_empty((rows, out), dtype=out_dtype)
+    pre = x.new_empty((rows, out), dtype=out_dtype) if keep_pre else None
+    _call(lib.ink_linear, x, x.data_ptr(), ld, weight.data_ptr(), ld_w, _ptr(bias), _ptr(residual), ld_res, rows, cols, out, TYPES[t],
+          TYPES[out_dtype], ACTS[act], y.data_ptr(), out, _ptr(pre), out)
     return (y, pre) if keep_pre else y
 
 
 def linear_backward(dy, x, weight, pre=None, act="none", need_dx=True, need_dweight=True, need_dbias=True):
     """(dx, dweight, dbias) of linear, in the rows' type; None for what is not needed.  dy and pre (what linear kept, not
     needed for act "none") have x's type, or float32 with bfloat16 rows.  The gradient of the residual is dy."""
-    x = _matrix(x, "x")
+    x, ld = _matrix(x, "x")
     rows, cols = x.shape
-    weight = _matrix(weight, "weight", cols, None, x.dtype, x)
+    t = x.dtype
+    weight, ld_w = _matrix(weight, "weight", cols, None, t, x)
     out = weight.shape[1]
-    dy = _matrix(dy, "dy", rows, out, None, x)
-    if dy.dtype != x.dtype and not (dy.dtype == torch.float32 and x.dtype == torch.bfloat16):
-        raise TypeError("dy has type %s, the rows %s: wanted the same, or float32 with bfloat16 rows" % (dy.dtype, x.dtype))
+    dy, ld_dy = _matrix(dy, "dy", rows, out, None, x)
+    if dy.dtype is not t and not (dy.dtype is torch.float32 and t is torch.bfloat16):
+        raise TypeError("dy has type %s, the rows %s: wanted the same, or float32 with bfloat16 rows" % (dy.dtype, t))
     if act not in ACTS:
         raise ValueError("act must be one of %s" % ", ".join(ACTS))
+    ld_pre = 0
     if act == "none":
         pre = None
     else:
-        pre = _matrix(pre, "pre", rows, out, dy.dtype, x)
+        pre, ld_pre = _matrix(pre, "pre", rows, out, dy.dtype, x)
     lib = _functions()
-    dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if need_dx else None
-    dweight = torch.empty((cols, out), dtype=x.dtype, device=x.device) if need_dweight else None
-    dbias = torch.empty(out, dtype=x.dtype, device=x.device) if need_dbias else None
+    dx = x.new_empty((rows, cols)) if need_dx else None
+    dweight = x.new_empty((cols, out)) if need_dweight else None
+    dbias = x.new_empty(out) if need_dbias else None
     n_work = lib.ink_linear_backward_work(rows, cols, out) if need_dweight or need_dbias else 0
-    work = torch.empty(n_work, dtype=torch.uint8, device=x.device) if n_work else None
-    with _on(x):
-        _check(lib, lib.ink_linear_backward(dy.data_ptr(), dy.stride(0), x.data_ptr(), x.stride(0), weight.data_ptr(), weight.stride(0),
-                                            _ptr(pre), 0 if pre is None else pre.stride(0), rows, cols, out, TYPES[x.dtype],
-                                            TYPES[dy.dtype], ACTS[act], _ptr(dx), cols, _ptr(dweight), out, _ptr(dbias), _ptr(work),
-                                            n_work, _stream(x)))
+    work = x.new_empty(n_work, dtype=torch.uint8) if n_work else None
+    _call(lib.ink_linear_backward, x, dy.data_ptr(), ld_dy, x.data_ptr(), ld, weight.data_ptr(), ld_w, _ptr(pre), ld_pre, rows, cols, out,
+          TYPES[t], TYPES[dy.dtype], ACTS[act], _ptr(dx), cols, _ptr(dweight), out, _ptr(dbias), _ptr(work), n_work)
     return dx, dweight, dbias
 
 
-def _targets(t, rows, like):
-    return None if t is None else _vector(t, "targets", rows, like, (torch.int64, torch.int32))
+_INTEGERS = (torch.int64, torch.int32)
 
 
 def log_probs(logits, targets=None, top=0, scale=1.0):
     """Of each row of logits, with p = softmax(scale * logits): dict of logp (log p of the row's target; 0 where the target is
     no class, -1 for instance), entropy, lse (all [rows] float32), and the `top` best classes: top_ids (int32) and
     top_logp, both [rows, top], best first and equal logits by the lower class."""
-    logits = _matrix(logits, "logits")
+    logits, ld = _matrix(logits, "logits")
     rows, classes = logits.shape
-    targets = _targets(targets, rows, logits)
+    targets = _vector(targets, "targets", rows, logits, _INTEGERS)
     if not 0 <= top <= min(classes, MAX_TOP):
         raise ValueError("top must be 0 .. min(classes, %d)" % MAX_TOP)
-    lib, dev, t = _functions(), logits.device, TYPES[logits.dtype]
-    logp, entropy, lse = (torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(3))
-    ids = torch.empty((rows, top), dtype=torch.int32, device=dev)
-    top_logp = torch.empty((rows, top), dtype=torch.float32, device=dev)
+    lib, t = _functions(), TYPES[logits.dtype]
+    logp, entropy, lse = logits.new_empty((3, rows), dtype=torch.float32).unbind(0)
+    ids = logits.new_empty((rows, top), dtype=torch.int32)
+    top_logp = logits.new_empty((rows, top), dtype=torch.float32)
     n_work = lib.ink_log_probs_work(rows, classes, t, top)
-    work = torch.empty(n_work, dtype=torch.uint8, device=dev) if n_work else None
-    with _on(logits):
-        _check(lib, lib.ink_log_probs(logits.data_ptr(), logits.stride(0), _ptr(targets), 0 if targets is None else targets.element_size(),
-                                      rows, classes, t, scale, top, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), ids.data_ptr(),
-                                      top_logp.data_ptr(), _ptr(work), n_work, _stream(logits)))
+    work = logits.new_empty(n_work, dtype=torch.uint8) if n_work else None
+    at = logp.data_ptr()
+    _call(lib.ink_log_probs, logits, logits.data_ptr(), ld, _ptr(targets), 0 if targets is None else targets.element_size(), rows, classes, t,
+          scale, top, at, at + 4 * rows, at + 8 * rows, ids.data_ptr(), top_logp.data_ptr(), _ptr(work), n_work)
     return dict(logp=logp, entropy=entropy, lse=lse, top_ids=ids, top_logp=top_logp)
 
 
 def log_probs_backward(logits, targets, lse, entropy=None, g_logp=None, g_entropy=None, scale=1.0):
     """Gradient by the logits of sum(g_logp * logp) + sum(g_entropy * entropy), in the logits' type.  lse and entropy are
     log_probs'; either gradient may be None (entropy is needed with g_entropy)."""
-    logits = _matrix(logits, "logits")
+    logits, ld = _matrix(logits, "logits")
     rows, classes = logits.shape
-    targets = _targets(targets, rows, logits)
-    f32 = (torch.float32,)
-    lse = _vector(lse, "lse", rows, logits, f32)
-    entropy, g_logp, g_entropy = (None if v is None else _vector(v, n, rows, logits, f32)
-                                  for v, n in ((entropy, "entropy"), (g_logp, "g_logp"), (g_entropy, "g_entropy")))
+    targets = _vector(targets, "targets", rows, logits, _INTEGERS)
+    lse, entropy = _vector(_given(lse, "lse"), "lse", rows, logits, _F32), _vector(entropy, "entropy", rows, logits, _F32)
+    g_logp, g_entropy = _vector(g_logp, "g_logp", rows, logits, _F32), _vector(g_entropy, "g_entropy", rows, logits, _F32)
     lib = _functions()
-    out = torch.empty((rows, classes), dtype=logits.dtype, device=logits.device)
-    with _on(logits):
-        _check(lib, lib.ink_log_probs_backward(logits.data_ptr(), logits.stride(0), _ptr(targets),
-                                               0 if targets is None else targets.element_size(), lse.data_ptr(), _ptr(entropy),
-                                               _ptr(g_logp), _ptr(g_entropy), rows, classes, TYPES[logits.dtype], scale, out.data_ptr(),
-                                               classes, _stream(logits)))
+    out = logits.new_empty((rows, classes))
+    _call(lib.ink_log_probs_backward, logits, logits.data_ptr(), ld, _ptr(targets), 0 if targets is None else targets.element_size(),
+          lse.data_ptr(), _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), rows, classes, TYPES[logits.dtype], scale, out.data_ptr(), classes)
     return out
