@@ -406,28 +406,15 @@ __global__ __launch_bounds__(kWave * WN * WM * WK, PER) void k_linear_stream(Str
   constexpr int VK = kVec<T>, THREADS = kWave * WN * WM * WK, MR = 32 * WM, NT = NTW * WN, BN = 32 * NT, STEPS = KS * WK;
   constexpr int P = STEPS * 32 + 16;         // bytes between rows in LDS: 16 lanes' pieces fall on all banks
   constexpr int NL = (MR * 2 * STEPS + THREADS - 1) / THREADS;
-  constexpr int OE = 16 / sizeof(TO), NO = (MR * BN / OE + THREADS - 1) / THREADS, PS = 4, PART = MR * (BN + 4);
-  static_assert(STEPS % PS == 0, "whole pieces");
+  constexpr int OE = 16 / sizeof(TO), NO = (MR * BN / OE + THREADS - 1) / THREADS, PART = MR * (BN + 4);
+  constexpr int ROOM = MR * P + WK * PART * 4, STEP_BYTES = BN * 32;       // W goes through the same LDS, in as few pieces as it takes
+  constexpr int PS = STEPS * STEP_BYTES <= ROOM ? STEPS : STEPS / 2 * STEP_BYTES <= ROOM ? STEPS / 2 : 4;
+  static_assert(STEPS % PS == 0 && PS * STEP_BYTES <= ROOM, "whole pieces");
   extern __shared__ __align__(16) char s_mem[];
   char *s_x = s_mem;
   float *s_o = reinterpret_cast<float *>(s_mem + MR * P), *s_b = s_o + WK * PART;
   const int tid = threadIdx.x, l = lane_id(), half = l / 32, wave = tid / kWave, wn = wave % WN, wm = wave / WN % WM, wk = wave / (WN * WM);
   const int n0 = blockIdx.y * BN, width = min(BN, a.width - n0);
-  V w[KS][NTW];
-#pragma unroll
-  for (int k0 = 0; k0 < STEPS; k0 += PS) {
-    __syncthreads();
-    stage_weights<T, NT, GRAD>(a, reinterpret_cast<V *>(s_mem), k0 * kStep<T>, PS * kStep<T>, n0);
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < PS; s++)
-      if (WK == 1 || wk == (k0 + s) / KS)
-#pragma unroll
-        for (int i = 0; i < NTW; i++) w[(k0 + s) % KS][i] = reinterpret_cast<V *>(s_mem)[(s * NT + wn * NTW + i) * 64 + l];
-  }
-  __syncthreads();
-  for (int i = tid; i < MR * P / 16; i += THREADS) reinterpret_cast<V *>(s_x)[i] = V{};      // past the depth it stays zero
-  for (int i = tid; i < BN; i += THREADS) s_b[i] = !GRAD && a.bias && i < width ? (float)static_cast<const T *>(a.bias)[n0 + i] : 0.f;
   const int64_t tiles = (a.rows + MR - 1) / MR;
   const bool narrow = a.depth < VK;
   // This thread's pieces of a tile of rows: place in LDS, and offsets from the tile's first row, the same for every tile.
@@ -510,7 +497,22 @@ __global__ __launch_bounds__(kWave * WN * WM * WK, PER) void k_linear_stream(Str
     return reinterpret_cast<decltype(base)>(reinterpret_cast<Byte *>(base) + (__umul24(out_row[j], (uint32_t)ld) + out_col[j]) * (uint32_t)sizeof(TO));
   };
   int64_t t = blockIdx.x;
-  if (t < tiles) fetch(t);
+  if (t < tiles) fetch(t);                   // on its way while W is laid out
+  V w[KS][NTW];
+#pragma unroll
+  for (int k0 = 0; k0 < STEPS; k0 += PS) {
+    __syncthreads();
+    stage_weights<T, NT, GRAD>(a, reinterpret_cast<V *>(s_mem), k0 * kStep<T>, PS * kStep<T>, n0);
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < PS; s++)
+      if (WK == 1 || wk == (k0 + s) / KS)
+#pragma unroll
+        for (int i = 0; i < NTW; i++) w[(k0 + s) % KS][i] = reinterpret_cast<V *>(s_mem)[(s * NT + wn * NTW + i) * 64 + l];
+  }
+  __syncthreads();
+  for (int i = tid; i < MR * P / 16; i += THREADS) reinterpret_cast<V *>(s_x)[i] = V{};      // past the depth it stays zero
+  for (int i = tid; i < BN; i += THREADS) s_b[i] = !GRAD && a.bias && i < width ? (float)static_cast<const T *>(a.bias)[n0 + i] : 0.f;
   __syncthreads();                           // the zeros are there
   for (; t < tiles; t += gridDim.x) {
     put();
@@ -890,6 +892,7 @@ __global__ __launch_bounds__(256) void k_grad_sum(GradSumArgs a) {
   const int64_t i = ((int64_t)(bias ? blockIdx.x - a.weight_groups : blockIdx.x) * 16 + x) * 4;
   F4 t = F4{};
   if (i < n)
+#pragma unroll 8
     for (int p = y; p < a.slices; p += 16) t += *reinterpret_cast<const F4 *>(part + p * n + i);
   s[y][x] = t;
   __syncthreads();

@@ -192,6 +192,7 @@ __global__ __launch_bounds__(1024) void k_norm_params(const float *part, int n_p
   const int x = threadIdx.x % 32, y = threadIdx.x / 32, c = blockIdx.x * 32 + x;
   float t = 0.f;
   if (c < cols)
+#pragma unroll 8
     for (int i = y; i < n_part; i += 32) t += part[(int64_t)i * 2 * cols + blockIdx.y * cols + c];
   s[y][x] = t;
   __syncthreads();
