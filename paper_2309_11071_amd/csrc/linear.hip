@@ -636,8 +636,8 @@ __global__ __launch_bounds__(kHeadThreads) void k_linear_few(LinearArgs a) {
 
 // ------------------------------------------------------------------------------------ gradient
 // dweight = x^T dz and dbias over a slice of the rows, and (DX) dx = dz W^T of its rows on the way, so that dy, z and x are read once.
-// A workgroup has the sums of 32 KT columns of x by 32 NT of dz in registers, (KT / 2) (NT / 2) tiles a wave, and takes 32 rows at a time, one
-// piece ahead in registers.  All threads load x, dy and z side by side, 16 bytes a lane, form dz once and put both into LDS row by row.  The
+// A workgroup has the sums of 32 KT columns of x by 32 NT of dz in registers, (KT / 2) (NT / 2) tiles a wave, and takes 32 rows at a time
+// (64 with eight waves, which larger tiles take), one piece ahead in registers.  All threads load x, dy and z side by side, 16 bytes a lane, form dz once and put both into LDS row by row.  The
 // sums run over the rows, so their fragments are columns: 16-bit ones come from the transposing LDS read, 32-bit ones element by
 // element.  The partial sums are left in the fragments' order and k_grad_sum puts them where they belong.
 struct GradArgs {
@@ -647,7 +647,7 @@ struct GradArgs {
   int64_t rows, ld_x, ld_dy, ld_pre, ld_w, ld_dx, slice;
   int cols, out, act;
 };
-constexpr int kGradRows = 32, kGradThreads = 256;
+constexpr int kGradRows = 32;                // rows that a slice is a multiple of
 
 // Bytes between rows in LDS: rows of 16 lanes' pieces fall on all banks, and in 32 bits two rows side by side nearly so.
 template <class T, int TILES> constexpr int kGradPitch = TILES * 32 * (int)sizeof(T) + (sizeof(T) == 2 ? 16 : 144);
@@ -671,18 +671,20 @@ template <class T> __device__ __forceinline__ typename Frag<T>::V columns_frag(c
   }
 }
 
-template <class T, class TI, int KT, int NT, bool DX>
-__global__ __launch_bounds__(kGradThreads, 2) void k_linear_grad(GradArgs a) {
+template <class T, class TI, int KT, int NT, int WAVES, bool DX>
+__global__ __launch_bounds__(kWave * WAVES, 2) void k_linear_grad(GradArgs a) {
   typedef typename Frag<T>::V V;
-  constexpr int VK = kVec<T>, STEPS = kGradRows / kStep<T>, CX = KT * 32 / VK, CZ = NT * 32 / VK;      // pieces of a row
-  constexpr int NX = kGradRows * CX / kGradThreads, NZ = kGradRows * CZ / kGradThreads;
-  constexpr int KP = KT / 2, NP = NT / 2, DP = (KT + 3) / 4, DS = CZ / 2;      // tiles a wave; column tiles of dx a wave, steps of its depth
+  constexpr int ROWS = 8 * WAVES, THREADS = kWave * WAVES, WN = WAVES / 2;     // waves: two by the columns of x, WN by those of dz
+  constexpr int VK = kVec<T>, STEPS = ROWS / kStep<T>, CX = KT * 32 / VK, CZ = NT * 32 / VK;      // pieces of a row
+  constexpr int NX = ROWS * CX / THREADS, NZ = ROWS * CZ / THREADS;
+  constexpr int KP = KT / 2, NP = NT / WN, DP = (KT + WAVES - 1) / WAVES, DS = CZ / 2;      // tiles a wave; column tiles of dx a wave, steps of its depth
   constexpr int PX = kGradPitch<T, KT>, PZ = kGradPitch<T, NT>, PD = KT * 32 + 4, PB = NT * 32 + 4;
-  constexpr int kLds = kGradRows * (PX + PZ + (DX ? PD * 4 : 0)), kLdsBias = kGradRows * PB * 4;
+  constexpr int kLds = ROWS * (PX + PZ + (DX ? PD * 4 : 0)), kLdsBias = ROWS * PB * 4;
+  static_assert(KT % 2 == 0 && NT % WN == 0 && (!DX || WAVES == 4), "every wave has its tiles; dx is formed of 32 rows");
   __shared__ __align__(16) char s_mem[kLds > kLdsBias ? kLds : kLdsBias];
-  __shared__ __align__(16) float s_db[NZ * VK > 16 ? kGradRows * PB : 1];
-  char *s_x = s_mem, *s_z = s_mem + kGradRows * PX;
-  float *s_dx = reinterpret_cast<float *>(s_z + kGradRows * PZ);
+  __shared__ __align__(16) float s_db[NZ * VK > 16 ? ROWS * PB : 1];
+  char *s_x = s_mem, *s_z = s_mem + ROWS * PX;
+  float *s_dx = reinterpret_cast<float *>(s_z + ROWS * PZ);
   const int tid = threadIdx.x, l = lane_id(), half = l / 32, wave = tid / kWave;
   const int k0 = blockIdx.x * (KT * 32), n0 = blockIdx.y * (NT * 32);
   const int64_t r_begin = blockIdx.z * a.slice, r_end = min(r_begin + a.slice, a.rows);
@@ -693,7 +695,7 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_linear_grad(GradArgs a) {
     for (int i = 0; i < DP; i++)
 #pragma unroll
       for (int s = 0; s < DS; s++) {
-        const int k = (wave + 4 * i) * 32 + l % 32, n = s * kStep<T> + half * VK;
+        const int k = (wave + WAVES * i) * 32 + l % 32, n = s * kStep<T> + half * VK;
         w[i][s] = V{};
         if (k < a.cols && n < a.out) w[i][s] = row_frag<T>(static_cast<const T *>(a.weight) + (int64_t)k * a.ld_w, n, a.out);
       }
@@ -746,9 +748,9 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_linear_grad(GradArgs a) {
         }
       }
     }
-    xp += kGradRows * a.ld_x;
-    yp += kGradRows * a.ld_dy;
-    zp += kGradRows * a.ld_pre;
+    xp += ROWS * a.ld_x;
+    yp += ROWS * a.ld_dy;
+    zp += ROWS * a.ld_pre;
   };
   auto put = [&](int64_t left) {
 #pragma unroll
@@ -787,10 +789,10 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_linear_grad(GradArgs a) {
     }
   };
   if (r_begin < r_end) fetch(r_end - r_begin);
-  for (int64_t r0 = r_begin; r0 < r_end; r0 += kGradRows) {
+  for (int64_t r0 = r_begin; r0 < r_end; r0 += ROWS) {
     put(r_end - r0);
     __syncthreads();
-    if (r0 + kGradRows < r_end) fetch(r_end - r0 - kGradRows);
+    if (r0 + ROWS < r_end) fetch(r_end - r0 - ROWS);
 #pragma unroll
     for (int s = 0; s < STEPS; s++) {
       V zs[NP], xs[KP];
@@ -803,20 +805,20 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_linear_grad(GradArgs a) {
     if constexpr (DX) {
 #pragma unroll
       for (int i = 0; i < DP; i++) {
-        if (wave + 4 * i >= KT) continue;
+        if (wave + WAVES * i >= KT) continue;
         f32x16 d = f32x16{};
 #pragma unroll
         for (int s = 0; s < DS; s++) d = mma(w[i][s], *reinterpret_cast<const V *>(s_z + l % 32 * PZ + (2 * s + half) * 16), d);
 #pragma unroll
         for (int e = 0; e < 4; e++) {
           const F4 v = {d[4 * e], d[4 * e + 1], d[4 * e + 2], d[4 * e + 3]};
-          *reinterpret_cast<F4 *>(s_dx + (l % 32) * PD + (wave + 4 * i) * 32 + 8 * e + 4 * half) = v;
+          *reinterpret_cast<F4 *>(s_dx + (l % 32) * PD + (wave + WAVES * i) * 32 + 8 * e + 4 * half) = v;
         }
       }
     }
     __syncthreads();
     if constexpr (DX) {
-      const int rows = (int)min((int64_t)kGradRows, r_end - r0);
+      const int rows = (int)min((int64_t)ROWS, r_end - r0);
 #pragma unroll
       for (int j = 0; j < NX; j++) {
         const int c = (my_piece + 8 * j) * VK;
@@ -867,11 +869,11 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_linear_grad(GradArgs a) {
       if (c < a.out && e >= over && c - over + e < a.out) s_sum[my_row * PB + cb * VK + e - over] = own[j][e];
   }
   __syncthreads();
-  for (int c = tid; c < NT * 32; c += kGradThreads) {
+  for (int c = tid; c < NT * 32; c += THREADS) {
     if (n0 + c >= a.out) continue;
     float t = 0.f;
 #pragma unroll
-    for (int r = 0; r < kGradRows; r++) t += s_sum[r * PB + c];
+    for (int r = 0; r < ROWS; r++) t += s_sum[r * PB + c];
     a.part_bias[((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * (NT * 32) + c] = t;
   }
 }
@@ -914,7 +916,8 @@ __global__ __launch_bounds__(256) void k_grad_sum(GradSumArgs a) {
 }
 
 // ------------------------------------------------------------------------------------ host side
-constexpr int64_t kFewRows = 16;
+constexpr int64_t kFewRows = 16;             // rows that a workgroup takes one by one: W is read from the caches for each
+constexpr int64_t kStreamRows = 32 * 1024;   // rows from which on a workgroup that lays out W for itself takes several tiles
 template <class T, class TI, class TO, int KS, int NTW, int WN, int WM, int WK, int PER, bool GRAD>
 static void stream_launch(const LinearArgs &a, Launches &run) {
   constexpr int MR = 32 * WM, BN = 32 * NTW * WN, OE = 16 / (int)sizeof(TO), WAVES = WN * WM * WK;
@@ -933,7 +936,7 @@ static void stream_launch(const LinearArgs &a, Launches &run) {
 }
 // whether the rows are so many that a workgroup takes several tiles, and W fits the registers
 template <class T, class TI, class TO, bool GRAD> static bool stream_run(const LinearArgs &a, Launches &run) {
-  if (a.rows < 32 * 1024) return false;
+  if (a.rows < kStreamRows) return false;
   for (const int64_t ld : {a.ld_in, a.ld_pre, a.ld_res, a.ld_out, a.ld_keep})
     if (ld >= 1 << 22) return false;         // offsets within a tile are 32-bit
   const int steps = (a.depth + kStep<T> - 1) / kStep<T>;
@@ -979,20 +982,29 @@ template <class T, class TI, class TO, bool GRAD> static void linear_run(const L
   run(ntw == 1 ? k_linear_tile<T, TI, TO, 1, GRAD> : k_linear_tile<T, TI, TO, 2, GRAD>, grid, dim3(256), a);
 }
 
-// How the gradient's sums are cut: tiles of 32 kt columns by 32 nt of dz, and slices of the rows, two workgroups a CU.
-struct GradPlan { int kt, nt, tiles_k, tiles_n, slices; int64_t slice, part, part_bias; bool whole; };
-static GradPlan grad_plan(int64_t rows, int cols, int out) {
+// How the gradient's sums are cut: tiles of 32 kt columns by 32 nt of dz, and slices of the rows, two workgroups of four waves a CU or one
+// of eight.  `wide`: 16-bit rows, whose registers leave room for tiles of 256 columns of x; dy and z, read again for every such tile, are
+// then read half as often.  bf16, four waves and eight: 612k x 256 x 256 with gelu 695 and 604 us, 612k x 256 x 100 330 and 297, 100k x 1000 x 500
+// 820 and 764, but 128 x 256 (one tile of x either way) 402 and 408, and 10000 rows 39 and 46.
+struct GradPlan { int kt, nt, waves, tiles_k, tiles_n, slices; int64_t slice, part, part_bias; bool whole; };
+static GradPlan grad_plan(int64_t rows, int cols, int out, bool wide) {
   GradPlan p{};
   const int k = (cols + 31) / 32, n = (out + 31) / 32;
+  p.waves = 4;
   p.kt = k <= 2 ? 2 : k <= 4 || n > 2 ? 4 : 8;
-  p.nt = n <= 2 ? 2 : n <= 4 || p.kt > 4 ? 4 : n <= 6 ? 6 : 4;
-  if (p.kt == 8) p.nt = 2;
+  p.nt = p.kt == 8 || n <= 2 ? 2 : n <= 4 ? 4 : n <= 6 ? 6 : 4;
+  if (wide && rows >= kStreamRows && k > 4 && n > 2) {
+    p.waves = 8;
+    p.kt = 8;
+    p.nt = n > 4 ? 8 : 4;
+  }
   p.tiles_k = (k + p.kt - 1) / p.kt;
   p.tiles_n = (n + p.nt - 1) / p.nt;
   p.whole = p.tiles_k == 1 && p.tiles_n == 1;
-  const int64_t blocks = (rows + kGradRows - 1) / kGradRows, tiles = (int64_t)p.tiles_k * p.tiles_n;
-  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>((blocks + 1) / 2, 512 / tiles));
-  p.slice = (blocks + slices - 1) / slices * kGradRows;
+  const int per = 8 * p.waves;               // rows at a time
+  const int64_t blocks = (rows + per - 1) / per, tiles = (int64_t)p.tiles_k * p.tiles_n;
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>((blocks + 1) / 2, 2048 / p.waves / tiles));
+  p.slice = (blocks + slices - 1) / slices * per;
   p.slices = (int)((rows + p.slice - 1) / p.slice);
   p.part = p.slices * tiles * p.kt * p.nt * 1024;
   p.part_bias = (int64_t)p.slices * p.tiles_n * p.nt * 32;
@@ -1002,10 +1014,15 @@ static GradPlan grad_plan(int64_t rows, int cols, int out) {
 template <class T, class TI, int KT, int NT> static void grad_launch(const GradArgs &a, const GradPlan &p, Launches &run) {
   const dim3 grid(p.tiles_k, p.tiles_n, p.slices);
   if constexpr (sizeof(T) == sizeof(TI) && (sizeof(T) == 2 || NT <= 4))
-    if (a.dx) return run(k_linear_grad<T, TI, KT, NT, true>, grid, dim3(kGradThreads), a);
-  run(k_linear_grad<T, TI, KT, NT, false>, grid, dim3(kGradThreads), a);
+    if (a.dx) return run(k_linear_grad<T, TI, KT, NT, 4, true>, grid, dim3(kWave * 4), a);
+  run(k_linear_grad<T, TI, KT, NT, 4, false>, grid, dim3(kWave * 4), a);
 }
 template <class T, class TI> static void grad_run(const GradArgs &a, const GradPlan &p, Launches &run) {
+  if constexpr (sizeof(T) == 2 && sizeof(TI) == 2)
+    if (p.waves == 8) {
+      const dim3 grid(p.tiles_k, p.tiles_n, p.slices), block(kWave * 8);
+      return run(p.nt == 8 ? k_linear_grad<T, TI, 8, 8, 8, false> : k_linear_grad<T, TI, 8, 4, 8, false>, grid, block, a);
+    }
   if (p.kt == 8) return grad_launch<T, TI, 8, 2>(a, p, run);
   if (p.kt == 2) {
     if (p.nt == 2) return grad_launch<T, TI, 2, 2>(a, p, run);
@@ -1055,8 +1072,8 @@ extern "C" ink_status ink_linear(const void *x, int64_t ld_x, const void *weight
 
 extern "C" size_t ink_linear_backward_work(int64_t rows, int32_t cols, int32_t out) {
   if (rows < 1 || rows > kMaxHeadRows || cols < 1 || cols > INK_MAX_IN_DIM || out < 1 || out > INK_MAX_IN_DIM) return 0;
-  const GradPlan p = grad_plan(rows, cols, out);
-  return (size_t)(p.part + p.part_bias) * sizeof(float);
+  const GradPlan p = grad_plan(rows, cols, out, false), q = grad_plan(rows, cols, out, true);     // enough for every type
+  return (size_t)std::max(p.part + p.part_bias, q.part + q.part_bias) * sizeof(float);
 }
 
 extern "C" ink_status ink_linear_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const void *weight, int64_t ld_w,
@@ -1079,9 +1096,9 @@ extern "C" ink_status ink_linear_backward(const void *dy, int64_t ld_dy, const v
     return fail_call(INK_E_ARG, "%s: work holds less than ink_linear_backward_work bytes or is not aligned to 16", who);
   Launches run(hip_stream);
   GradPlan p{};
-  if (rows > 0) p = grad_plan(rows, cols, out);
+  if (rows > 0) p = grad_plan(rows, cols, out, type != INK_F32 && type == dy_type);
   // dx in the same pass where one workgroup has all columns of both matrices and, in 32 bits, the registers for it
-  const bool sums = dweight || dbias, together = dx && sums && rows > 0 && p.whole && type == dy_type && (type != INK_F32 || p.nt <= 4);
+  const bool sums = dweight || dbias, together = dx && sums && rows > 0 && p.whole && p.waves == 4 && type == dy_type && (type != INK_F32 || p.nt <= 4);
   if (act == INK_ACT_NONE) pre = nullptr;
   if (dx && rows > 0 && !together) {
     LinearArgs a{};

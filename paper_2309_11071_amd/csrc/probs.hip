@@ -304,24 +304,20 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
         if (__any(vm >= floor_z)) {
 #pragma unroll
           for (int j = 0; j < V; j++) {
-            const bool live = at + j >= first && first < c1;
-            const uint32_t o = live && z[j] >= floor_z ? order_of_number(f[j]) : 0u;
-            if constexpr (EXACT) {
-              const uint32_t number = o ? (o & ~low) | (low - (uint32_t)(step * V + j)) : 0u;
-              if (__any(number > list[KS - 1])) put_number<KS>(list, number);
-            } else if (__any(o > best.o[KS - 1])) best.put(o, (int32_t)(at + j));
+            if (!__any(z[j] >= floor_z)) continue;
+            const uint32_t o = at + j >= first && first < c1 && z[j] >= floor_z ? order_of_number(f[j]) : 0u;
+            if constexpr (EXACT) put_number<KS>(list, o ? (o & ~low) | (low - (uint32_t)(step * V + j)) : 0u);
+            else if (__any(o > best.o[KS - 1])) best.put(o, (int32_t)(at + j));
           }
         }
-        if (step + 1 == refresh) {           // at steps 1, 2, 4, ...: the K-th best of the lanes' best
+        if (step + 1 == refresh) {           // at steps 1, 2, 4, ...: what K of the lanes' best reach
           refresh *= 2;
-          uint32_t head = EXACT ? order_of_list(list[0]) : best.o[0], o = 0;
+          const uint32_t head = EXACT ? list[0] : best.o[0];
+          uint32_t o = 0;                    // the largest number of 16 bits (then zeros) that K heads reach, bit by bit
 #pragma unroll
-          for (int k = 0; k < K; k++) {
-            o = group_all<kWave>(head, [](uint32_t p, uint32_t p2) { return p > p2 ? p : p2; });
-            const uint64_t who = __ballot(head == o);
-            head = lane_id() == __ffsll((unsigned long long)who) - 1 ? 0u : head;
-          }
-          if (o) floor_z = of_order(o) * a.scale;
+          for (int bit = 31; bit >= 16; bit--)
+            if (__popcll(__ballot(head >= (o | 1u << bit))) >= K) o |= 1u << bit;
+          if (o > 0x007fffffu) floor_z = of_order(o) * a.scale;              // (above -inf)
         }
       }
     }
