@@ -106,31 +106,32 @@ template <int L, int K> __device__ __forceinline__ void take_best(Best<float, K>
   b.pop(c == id && b.o[0] == o);
 }
 
+// maximum of the logits, sum of e^(z - z_max) and of its products with (z - z_max) log2 e
 struct RowStats { float m, s, u; };
 __device__ __forceinline__ float safe_max(float m) { return m == -__builtin_inff() ? 0.f : m; }
 
-// e^(z - m) and its product with z - m; a masked class (z = -inf) adds nothing to either
-__device__ __forceinline__ void add_term(float z, float m, float &s, float &u) {
-  const float t = z - m, e = __builtin_amdgcn_exp2f(t * kLog2e);
+// adds a logit; scale2 = scale log2 e.  A masked class (-inf) adds nothing to either sum.
+__device__ __forceinline__ void add_term(float f, float m, float scale2, float &s, float &u) {
+  const float t = (f - m) * scale2, e = __builtin_amdgcn_exp2f(t);
   s += e;
   u = fmaf(fmaxf(t, -1e30f), e, u);
 }
-// sums over `from` relative to the maximum `to`
-__device__ __forceinline__ void rescale(RowStats &a, float to) {
-  const float d = safe_max(a.m) - to, f = a.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(d * kLog2e);
+// the sums relative to another maximum
+__device__ __forceinline__ void rescale(RowStats &a, float to, float scale2) {
+  const float d = (safe_max(a.m) - to) * scale2, f = a.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(d);
   a.u = f == 0.f ? 0.f : (a.u + a.s * d) * f;
   a.s *= f;
   a.m = to;
 }
 
+__device__ __forceinline__ float row_lse(float m, float s, float scale) { return s == 0.f ? -__builtin_inff() : m * scale + logf(s); }
+
 // what a row's statistics say, written by one lane
-__device__ __forceinline__ float finish_row(const ProbsArgs &a, int64_t r, float m, float s, float u, float z_target, bool has) {
+__device__ __forceinline__ void finish_row(const ProbsArgs &a, int64_t r, float s, float u, float lse, float z_target, bool has) {
   const bool none = s == 0.f;
-  const float ls = logf(s), lse = none ? -__builtin_inff() : m + ls;
   if (a.lse) a.lse[r] = lse;
-  if (a.entropy) a.entropy[r] = none ? 0.f : ls - u / s;
+  if (a.entropy) a.entropy[r] = none ? 0.f : logf(s) - u * kLn2 / s;
   if (a.logp) a.logp[r] = !has ? 0.f : none ? -__builtin_inff() : z_target - lse;
-  return lse;
 }
 __device__ __forceinline__ void write_top(const ProbsArgs &a, int64_t r, int j, float v, int32_t id, float lse) {
   const float z = v * a.scale;
@@ -145,6 +146,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_rows(ProbsArgs a) {
   constexpr bool EXACT = sizeof(T) == 2;     // a number holds order and class
   constexpr int KL = EXACT ? K : K + 1;      // ... or one more place says whether the last one is certain
   const int q = threadIdx.x % L, C = (int)a.classes;
+  const float scale2 = a.scale * kLog2e;
   const uint32_t low = (1u << (EXACT ? kIdBits<T> : a.id_bits)) - 1;
   for (int64_t r0 = (int64_t)blockIdx.x * G; r0 < a.rows; r0 += (int64_t)gridDim.x * G) {
     const int64_t mine = r0 + threadIdx.x / L;
@@ -159,33 +161,36 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_rows(ProbsArgs a) {
     uint32_t list[KL > 0 ? KL : 1];
 #pragma unroll
     for (int k = 0; k < KL; k++) list[k] = 0;
+    // all vectors but the last are whole (NV is the least that holds the row); of that one the rest repeats the vector before
+    const int last = ((NV - 1) * L + q) * V, last_at = min(last, C - V);
     float m = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-      const int first = (i * L + q) * V, at = min(first, C - V);
+      const int at = i + 1 < NV ? (i * L + q) * V : last_at;
 #pragma unroll
       for (int j = 0; j < V; j++) {
-        const bool live = at + j >= first;                 // the rest is a repetition of the vector before
-        m = fmaxf(m, live ? f[i][j] * a.scale : -__builtin_inff());
-        if constexpr (K > 0) put_number<KL>(list, live ? (order_of_number(f[i][j]) & ~low) | (low - (uint32_t)(at + j)) : 0u);
+        uint32_t number = 0;
+        if constexpr (K > 0) number = (order_of_number(f[i][j]) & ~low) | (low - (uint32_t)(at + j));
+        if (i + 1 == NV) {
+          const bool live = at + j >= last;
+          f[i][j] = live ? f[i][j] : -__builtin_inff();
+          number = live ? number : 0u;
+        }
+        m = fmaxf(m, f[i][j]);
+        if constexpr (K > 0) put_number<KL>(list, number);
       }
     }
-    m = group_all<L>(m, [](float p, float p2) { return fmaxf(p, p2); });
-    const float ms = safe_max(m);
+    m = safe_max(group_all<L>(m, [](float p, float p2) { return fmaxf(p, p2); }));
     float s = 0.f, u = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; i++)
 #pragma unroll
-      for (int j = 0; j < V; j++) {
-        const int first = (i * L + q) * V, at = min(first, C - V);
-        add_term(at + j >= first ? f[i][j] * a.scale : -__builtin_inff(), ms, s, u);
-      }
+      for (int j = 0; j < V; j++) add_term(f[i][j], m, scale2, s, u);
     s = group_sum<L>(s);
     u = group_sum<L>(u);
     const bool on = mine < a.rows;
-    float lse = 0.f;
-    if (on && q == 0) lse = finish_row(a, r, ms, s, u, zt, has);
-    else lse = s == 0.f ? -__builtin_inff() : ms + logf(s);
+    const float lse = row_lse(m, s, a.scale);
+    if (on && q == 0) finish_row(a, r, s, u, lse, zt, has);
     if constexpr (K > 0) {
       uint32_t o[KL];
       bool open = s != s;                    // a NaN (or +inf) in the row
@@ -271,6 +276,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
   __shared__ uint32_t s_o[(W + 1) * KS];
   __shared__ int32_t s_id[(W + 1) * KS];
   const int tid = threadIdx.x % TW;
+  const float scale2 = a.scale * kLog2e;
   for (int64_t item = (int64_t)blockIdx.x * G + threadIdx.x / TW; item < a.rows * a.parts; item += (int64_t)gridDim.x * G) {
     auto order_of_list = [](uint32_t number) { return number == 0 ? 0u : number & 0x80000000u ? number & ~low : number | low; };
     const int64_t r = item / a.parts;
@@ -283,29 +289,30 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
     uint32_t list[KS];
 #pragma unroll
     for (int k = 0; k < KS; k++) list[k] = 0;
-    float floor_z = -__builtin_inff();       // K elements of the wave are at least this large
+    float floor_f = -__builtin_inff();       // K elements of the wave are at least this large
     int64_t refresh = 1, step = 0;
     const int64_t n_vec = (c1 - c0 + V - 1) / V;
     for (int64_t i0 = 0; i0 < n_vec; i0 += TW, step++) {
       const int64_t first = c0 + (i0 + tid) * V, at = min(first, a.classes - V);
-      float f[V], z[V];
+      float f[V];
       load_pack<T, V>(x + at, f);
-      float vm = -__builtin_inff();
+      const bool whole = i0 + TW < n_vec;    // of the last vectors some repeat elements or are past the part
+      if (!whole)
 #pragma unroll
-      for (int j = 0; j < V; j++) {
-        z[j] = at + j >= first && first < c1 ? f[j] * a.scale : -__builtin_inff();
-        vm = fmaxf(vm, z[j]);
-      }
-      if (vm > st.m) rescale(st, vm);
+        for (int j = 0; j < V; j++) f[j] = at + j >= first && first < c1 ? f[j] : -__builtin_inff();
+      float vm = f[0];
+#pragma unroll
+      for (int j = 1; j < V; j++) vm = fmaxf(vm, f[j]);
+      if (vm > st.m) rescale(st, vm, scale2);
       const float ms = safe_max(st.m);
 #pragma unroll
-      for (int j = 0; j < V; j++) add_term(z[j], ms, st.s, st.u);
+      for (int j = 0; j < V; j++) add_term(f[j], ms, scale2, st.s, st.u);
       if constexpr (K > 0) {
-        if (__any(vm >= floor_z)) {
+        if (__any(vm >= floor_f)) {
 #pragma unroll
           for (int j = 0; j < V; j++) {
-            if (!__any(z[j] >= floor_z)) continue;
-            const uint32_t o = at + j >= first && first < c1 && z[j] >= floor_z ? order_of_number(f[j]) : 0u;
+            if (!__any(f[j] >= floor_f)) continue;
+            const uint32_t o = f[j] >= floor_f && (whole || (at + j >= first && first < c1)) ? order_of_number(f[j]) : 0u;
             if constexpr (EXACT) put_number<KS>(list, o ? (o & ~low) | (low - (uint32_t)(step * V + j)) : 0u);
             else if (__any(o > best.o[KS - 1])) best.put(o, (int32_t)(at + j));
           }
@@ -317,7 +324,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
 #pragma unroll
           for (int bit = 31; bit >= 16; bit--)
             if (__popcll(__ballot(head >= (o | 1u << bit))) >= K) o |= 1u << bit;
-          if (o > 0x007fffffu) floor_z = of_order(o) * a.scale;              // (above -inf)
+          if (o > 0x007fffffu) floor_f = of_order(o);        // (above -inf)
         }
       }
     }
@@ -330,7 +337,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
 #pragma unroll
       for (int w = 1; w < W; w++) bm = fmaxf(bm, s_m[w]);
     }
-    rescale(st, safe_max(bm));
+    rescale(st, safe_max(bm), scale2);
     float s = group_sum<kWave>(st.s), u = group_sum<kWave>(st.u);
     if constexpr (TW > kWave) {
       if (lane_id() == 0) { s_s[threadIdx.x / kWave] = s; s_u[threadIdx.x / kWave] = u; }
@@ -367,12 +374,11 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
         a.part_id[p * a.top + threadIdx.x] = s_id[W * KS + threadIdx.x];
       }
     } else {
-      const float ms = safe_max(bm);
-      const float lse = s == 0.f ? -__builtin_inff() : ms + logf(s);
+      const float lse = row_lse(safe_max(bm), s, a.scale);
       if (tid == 0) {
         const int64_t t = target_of(a.targets, a.wide_targets, r);
         const bool has = t >= 0 && t < a.classes;
-        finish_row(a, r, ms, s, u, has ? (float)x[t] * a.scale : 0.f, has);
+        finish_row(a, r, s, u, lse, has ? (float)x[t] * a.scale : 0.f, has);
       }
       if constexpr (K > 0) {
         uint32_t o = 0;
@@ -403,14 +409,14 @@ __global__ __launch_bounds__(kWave) void k_probs_join(ProbsArgs a) {
     RowStats st = {a.part_stats[3 * p], a.part_stats[3 * p + 1], a.part_stats[3 * p + 2]};
     if (l >= a.parts) st = {-__builtin_inff(), 0.f, 0.f};
     const float m = safe_max(group_all<kWave>(st.m, [](float x, float y) { return fmaxf(x, y); }));
-    rescale(st, m);
+    rescale(st, m, a.scale * kLog2e);
     const float s = group_sum<kWave>(st.s), u = group_sum<kWave>(st.u);
-    const float lse = s == 0.f ? -__builtin_inff() : m + logf(s);
+    const float lse = row_lse(m, s, a.scale);
     if (l == 0) {
       const T *x = static_cast<const T *>(a.logits) + r * a.ld;
       const int64_t t = target_of(a.targets, a.wide_targets, r);
       const bool has = t >= 0 && t < a.classes;
-      finish_row(a, r, m, s, u, has ? (float)x[t] * a.scale : 0.f, has);
+      finish_row(a, r, s, u, lse, has ? (float)x[t] * a.scale : 0.f, has);
     }
     if constexpr (K > 0) {
       Best<float, K> b;
@@ -505,6 +511,10 @@ template <class T, int L, int K> static void probs_rows(const ProbsArgs &a, Laun
   const int64_t n_vec = (a.classes + V - 1) / V, per = kHeadThreads / L;
   const dim3 grid((unsigned)std::min<int64_t>((a.rows + per - 1) / per, 16384));
   if (a.classes < V) { if constexpr (L == 8) run(k_probs_rows<T, 8, 1, 1, K>, grid, dim3(kHeadThreads), a); return; }
+  if constexpr (L == 2) {                    // (wider groups hold more than two vectors a lane)
+    if (n_vec <= L) return run(k_probs_rows<T, L, 1, V, K>, grid, dim3(kHeadThreads), a);
+    if (n_vec <= 2 * L) return run(k_probs_rows<T, L, 2, V, K>, grid, dim3(kHeadThreads), a);
+  }
   run(n_vec <= 3 * L ? k_probs_rows<T, L, 3, V, K> : k_probs_rows<T, L, 4, V, K>, grid, dim3(kHeadThreads), a);
 }
 
