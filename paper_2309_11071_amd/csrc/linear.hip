@@ -3,17 +3,23 @@
 //   forward   z = x W + bias (kept if asked for),  y = act(z) + residual
 //   gradient  dz = dy act'(z):  dx = dz W^T,  dweight = x^T dz,  dbias = sum over rows of dz
 //
-// W is [cols][out] as the layers' weights are.  The rows are many and both sides of W are short, so the product is bound by
-// reading the rows and writing the results wherever 16-bit types are used, and by the matrix unit in 32 bits.  A wave takes 32 rows and
-// all of a tile's columns: the rows go from memory straight into the registers that the matrix instructions read (lane = row,
-// 16 bytes a load), W is laid out in LDS in the order in which the lanes read it, once per workgroup where it fits.  The product
-// is formed transposed, W's columns as the instruction's rows, so that a lane ends up with four neighbouring columns of its row and stores
-// them together.
+// W is [cols][out] as the layers' weights are.  The rows are many and both sides of W are short, so 16-bit products are bound by
+// reading the rows and writing the results, 32-bit ones by the matrix unit.  Every product is formed transposed, W's columns as
+// the instruction's rows, so that a lane ends up with four neighbouring columns of its row.  Which kernel:
+//
+//   up to 64 rows               k_linear_few     a row and 32 columns a workgroup; W is what is read: 1 x 602 x 256 bf16 5 us
+//   from 32768 rows on          k_linear_stream  W in registers, rows in a stream; up to 640 terms (16 bits) or 256 (32 bits)
+//   enough rows for 256 tiles   k_linear_tile    128 rows by 64 or 128 columns
+//   else                        k_linear_small   32 by 32, eight waves share the depth: 100 x 602 x 256 f32 37 us in tiles, 11 (the call) so
+//
+// The stream against the tiles, in one run: 50k x 128 x 47 bf16 11 and 14 us, 200k x 128 x 128 26 and 40, 200k x 256 x 256 59 and 91; f32 of 128 x 64,
+// which the matrix unit holds up, 50k rows 19 and 19, 200k 49 and 54.
 //
 // Products are exact (16-bit operands) or fused (32 bits), and summed in 32 bits; the epilogue is in 32 bits and y, z, dx, dweight and
-// dbias are rounded once.  For 16-bit rows dz is rounded to the rows' type before the two products, which take 16-bit operands; dbias
-// sums the unrounded values.  dweight is a sum over all rows: workgroups take slices of the rows and leave a
-// partial matrix each, which k_weight_sum adds up in order (no atomics: the same call gives the same bits).
+// dbias are rounded once.  For 16-bit rows dz is rounded to the rows' type before the two products, which take 16-bit operands: an error
+// of the size of the results' own rounding, for half the matrix instructions of two 16-bit parts; dbias sums the unrounded values.  dweight is
+// a sum over all rows: workgroups take slices of the rows and leave a partial matrix each, which k_grad_sum adds up in order (no
+// atomics: the same call gives the same bits).
 #include <algorithm>
 #include <type_traits>
 
@@ -111,7 +117,7 @@ struct LinearArgs {
   const void *weight, *bias, *res;
   void *out, *keep;                          // forward: y, z or NULL; gradient: dx
   int64_t rows, ld_in, ld_pre, ld_w, ld_res, ld_out, ld_keep;
-  int depth, width, act, chunk;              // terms of a sum, columns of the result, elements of the depth in LDS at a time
+  int depth, width, act;                     // terms of a sum, columns of the result
 };
 
 // kVec elements k .. of one row of n elements as a fragment; past the row's end zeros, and nothing is read there.
@@ -192,8 +198,6 @@ template <class T> __device__ __forceinline__ void store4(T *p, int c, int n, co
   for (int j = 0; j < 4; j++)
     if (c + j < n) p[c + j] = (T)v[j];
 }
-
-constexpr int kLinearThreads = 512;
 
 // Four neighbouring columns of a row of results, from the registers of the products: bias, z, activation, residual, y.
 template <class T, class TO, bool GRAD> __device__ __forceinline__ void finish4(const LinearArgs &a, int64_t r, int c, float v[4]) {
@@ -385,8 +389,11 @@ __global__ __launch_bounds__(kWave * kSmallWaves) void k_linear_small(LinearArgs
 // Rows in a stream.  A workgroup of WM x WN waves holds W in registers for good: a wave has the fragments of its 32 NTW columns over
 // the whole depth (KS steps).  It takes 32 WM rows at a time: all threads load them side by side (16 bytes a lane, whole lines), a tile
 // ahead, and put them into LDS, from where every wave reads the fragments of its 32 rows; the product goes through
-// LDS in 32 bits once more, so that residual, z and y are read and written in whole lines too.  What a row costs beyond its bytes is
-// then little LDS traffic and one matrix instruction per 32 x 32 x kStep.
+// LDS in 32 bits once more, so that residual, z and y are read and written in whole lines too.  Bound by memory in 16 bits: 2.45M x 256 x
+// 256 with residual and z 1.0 ms (5.02 GB, 4.9 TB/s), without 0.59 (4.2), 2.45M x 128 x 64 167 us (5.6); the matrix unit is busy 15 % of the time.  In
+// 32 bits the matrix unit and memory take turns: 2.45M x 128 x 64 475 us, 85 TFLOP/s.  The group sizes are those that
+// leave the registers without spills (256 with two waves a SIMD) and were the fastest of those measured: 602 x 256 with a 20-step half
+// of the depth a wave 541 us, with all 40 steps of 32 columns 425; 602 x 47 split four ways 214, unsplit 363.
 struct StreamArgs {
   LinearArgs a;
   int chunks, pitch, flat;                   // 16-byte pieces of a row's depth; floats between rows of results in LDS; see emit
@@ -640,6 +647,8 @@ __global__ __launch_bounds__(kHeadThreads) void k_linear_few(LinearArgs a) {
 // (64 with eight waves, which larger tiles take), one piece ahead in registers.  All threads load x, dy and z side by side, 16 bytes a lane, form dz once and put both into LDS row by row.  The
 // sums run over the rows, so their fragments are columns: 16-bit ones come from the transposing LDS read, 32-bit ones element by
 // element.  The partial sums are left in the fragments' order and k_grad_sum puts them where they belong.
+// 612k x 128 x 172 bf16: without an activation 142 us (3.7 TB/s of the bytes it cannot do without), with gelu 198: the slope is formed once an
+// element, and its 25 instructions are what bounds that.
 struct GradArgs {
   const void *x, *dy, *pre, *weight;
   void *dx;
@@ -916,7 +925,8 @@ __global__ __launch_bounds__(256) void k_grad_sum(GradSumArgs a) {
 }
 
 // ------------------------------------------------------------------------------------ host side
-constexpr int64_t kFewRows = 16;             // rows that a workgroup takes one by one: W is read from the caches for each
+constexpr int64_t kFewRows = 64;             // rows that workgroups take one by one, W from the caches for each: bf16, 1 / 16 / 32 rows of
+                                             // 602 x 256 5.2 / 4.9 / 5.0 us, k_linear_small 8.4 / 8.4 / 8.5; 32 of 1024 x 1024 6.8 and 12.5
 constexpr int64_t kStreamRows = 32 * 1024;   // rows from which on a workgroup that lays out W for itself takes several tiles
 template <class T, class TI, class TO, int KS, int NTW, int WN, int WM, int WK, int PER, bool GRAD>
 static void stream_launch(const LinearArgs &a, Launches &run) {

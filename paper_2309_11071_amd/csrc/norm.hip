@@ -4,7 +4,8 @@
 //   gradient  h = (x - mean) rstd,  g = dy weight:   dx = rstd (g - mean(g) - h mean(g h)),
 //             dweight = sum over rows of dy h,  dbias = sum over rows of dy
 //
-// Both are bound by memory: eight to eleven operations an element against 4 to 12 bytes.  So a row is read once: L lanes hold it
+// Both are bound by memory, eight to eleven operations an element against 4 to 12 bytes, and run at the rate of a copy (5.0 TB/s):
+// 2.45M x 256 bf16 forward 504 us, 233k x 602 f32 gradient 340 us, 5 of them for the partial rows' sum.  So a row is read once: L lanes hold it
 // in registers, V elements (16 bytes) a load and NV loads a lane, and the variance is taken of the differences from the mean
 // without a second read.  L is the smallest group that holds a row with NV <= 4: the fewer lanes a row has, the fewer steps
 // its sums take and the more rows a wave has under way.  The last load of a row that is no multiple of V elements starts V
