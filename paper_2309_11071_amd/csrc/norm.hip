@@ -231,8 +231,10 @@ template <class T, int L, int V> static void norm_vectors(const NormArgs &a, int
     if (nv == 1) return norm_launch<T, L, 1, V, false>(a, grad, run);
     if (nv == 2) return norm_launch<T, L, 2, V, false>(a, grad, run);
   }
-  if (nv <= 3) return norm_launch<T, L, 3, V, false>(a, grad, run);
-  norm_launch<T, L, 4, V, false>(a, grad, run);
+  if constexpr (L != kWideThreads || INK_MAX_IN_DIM > 2 * V * L) {         // (16-bit rows of a workgroup have two vectors a thread at most)
+    if (nv <= 3) return norm_launch<T, L, 3, V, false>(a, grad, run);
+    norm_launch<T, L, 4, V, false>(a, grad, run);
+  }
 }
 
 template <class T> static void norm_dispatch(const NormArgs &a, bool grad, Launches &run) {

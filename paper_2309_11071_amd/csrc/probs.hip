@@ -555,10 +555,11 @@ template <class T, int L> static void grad_launch(const ProbsGradArgs &a, int nv
   constexpr int V = 16 / sizeof(T);
   const int64_t per = kHeadThreads / L, n = a.rows * a.chunks;
   const dim3 grid((unsigned)std::min<int64_t>((n + per - 1) / per, 1 << 20)), block(kHeadThreads);
-  if (nv == 1) run(k_probs_grad<T, L, 1, V>, grid, block, a);
-  else if (nv == 2) run(k_probs_grad<T, L, 2, V>, grid, block, a);
-  else if (nv == 3) run(k_probs_grad<T, L, 3, V>, grid, block, a);
-  else run(k_probs_grad<T, L, 4, V>, grid, block, a);
+  if constexpr (L == 4) {                    // (wider groups hold more than two vectors a lane)
+    if (nv == 1) return run(k_probs_grad<T, L, 1, V>, grid, block, a);
+    if (nv == 2) return run(k_probs_grad<T, L, 2, V>, grid, block, a);
+  }
+  run(nv <= 3 ? k_probs_grad<T, L, 3, V> : k_probs_grad<T, L, 4, V>, grid, block, a);
 }
 
 template <class T> static void grad_dispatch(ProbsGradArgs a, Launches &run) {

@@ -3,8 +3,9 @@ each with its gradient (include/ink.h has what they compute).
 
 Argument marshalling only: every operator runs inside libink.so.  Calls are asynchronous on torch's
 current stream of the tensors' device, like torch's own; results and work memory come from torch's
-allocator.  A matrix is a 2-D tensor whose rows are contiguous, at any distance from each other; any
-other layout is copied first.  Tensors of other devices or types and shapes that do not fit raise.
+allocator.  Nothing is recorded for autograd: the gradients are calls of their own.  A matrix is a 2-D
+tensor whose rows are contiguous, at any distance from each other; any other layout is copied first.
+Tensors of other devices or types and shapes that do not fit raise.
 """
 import ctypes as C
 
