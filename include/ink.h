@@ -361,12 +361,12 @@ ink_status ink_get_stats(ink_ctx *ctx, void *stats_out, size_t bytes);
  *
  * Matrices are row-major, of ink_type elements, row i at i * ld elements.  ld is any number from the
  * row's length up; a matrix that is read may also have ld = 0, one row for all.  Pointers need the alignment of an
- * element only.  No rows are allowed (outputs of whole-batch sums are then zeros).  Sums and statistics are kept in 32 bits,
+ * element only, work memory that of 16 bytes.  rows may be 0 (sums over the rows are then zeros).  Sums and statistics are kept in 32 bits,
  * outputs are rounded once, to nearest even.  NaN and infinities go where the formulas take them.
  * The order of a sum depends on the call's sizes: the same row in a call of other sizes may differ in the last bits.
  *
- * Errors: INK_E_ARG (NULL, misaligned or too little memory, sizes or types out of range, an unknown activation), INK_E_RANGE,
- * INK_E_DEVICE (a launch was refused); ink_last_error(NULL) has the message.  After an argument error nothing was enqueued. */
+ * Errors: INK_E_ARG (NULL, misaligned or too little memory, sizes or types out of range, an unknown activation; nothing was
+ * enqueued) and INK_E_DEVICE (a launch was refused); ink_last_error(NULL) has the message. */
 
 /* y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(var + eps), mean and (biased) variance of each row.
  *   x, y         [rows][cols] of `type`, cols 1 .. INK_MAX_IN_DIM
