@@ -411,7 +411,10 @@ ink_status ink_linear_backward(const void *dy, int64_t ld_dy, const void *x, int
  *   top_ids   [rows][top] the classes of the `top` largest logits, largest first; equal logits by the lower class, NaN
  *             first of all; top_logp [rows][top] their log p.  top 0 .. min(classes, INK_MAX_TOP)
  * Each output may be NULL.  targets: int32 (target_bytes 4) or int64 (8).  A class at -inf is masked.  In a row of masked
- * classes lse and every log p is -inf and the entropy 0; a NaN or +inf among the logits makes lse, entropy and log p NaN.
+ * classes lse and every log p is -inf and the entropy 0; a NaN or +inf among the logits makes lse, entropy and log p NaN.  Finite
+ * logits are numbers like others, a type's lowest among them, but for one further below its row's largest than a float can
+ * say (masked).  log p is formed of differences of logits and has its digits however far from zero these lie; where lse passes
+ * the range of float it is the largest finite number of its sign.
  *   scale     > 0 (1 / temperature);  classes 1 .. INK_MAX_CLASSES */
 size_t ink_log_probs_work(int64_t rows, int64_t classes, int32_t type, int32_t top);
 ink_status ink_log_probs(const void *logits, int64_t ld, const void *targets, int32_t target_bytes, int64_t rows, int64_t classes,

@@ -1,8 +1,11 @@
 // Log probabilities of given classes, entropy and the best alternatives of rows of logits, and the gradient.
 //
 //   z = scale * logit,  m = max z,  S = sum e^(z - m),  U = sum (z - m) e^(z - m)
-//   lse = m + log S,  log p_t = z_t - lse,  entropy = -sum p log p = log S - U / S
+//   lse = m + log S,  log p_t = (z_t - m) - log S,  entropy = -sum p log p = log S - U / S
 //   gradient of g log p_t + h entropy:  scale (g ([c = t] - p_c) - h p_c (log p_c + entropy))
+//
+// log p is a difference of logits and log S: formed of those it has the same digits wherever a row lies, which z - lse has near zero only
+// (47 logits near 20000: 1.2e-7 off, and 8.7e-4).  S, not lse, says whether a row has a class left.
 //
 // The alternatives are the classes of the largest logits, compared as they stand in memory: equal ones by the lower class, NaN
 // before everything, -0 equal to +0.  A class at -inf is masked (p = 0); a row of masked classes has lse = log p = -inf, entropy
@@ -127,19 +130,23 @@ __device__ __forceinline__ void rescale(RowStats &a, float to, float scale2) {
   a.m = to;
 }
 
-__device__ __forceinline__ float row_lse(float m, float s, float scale) { return s == 0.f ? -__builtin_inff() : m * scale + logf(s); }
-
-// what a row's statistics say, written by one lane
-__device__ __forceinline__ void finish_row(const ProbsArgs &a, int64_t r, float s, float u, float lse, float z_target, bool has) {
-  const bool none = s == 0.f;
-  if (a.lse) a.lse[r] = lse;
-  if (a.entropy) a.entropy[r] = none ? 0.f : logf(s) - u * kLn2 / s;
-  if (a.logp) a.logp[r] = !has ? 0.f : none ? -__builtin_inff() : z_target - lse;
+// log p of a logit of a row with maximum m (safe_max's) and log_s = log S, which is -inf where every class is masked
+__device__ __forceinline__ float log_p(float logit, float m, float log_s, float scale) {
+  return log_s == -__builtin_inff() ? log_s : (logit - m) * scale - log_s;
 }
-__device__ __forceinline__ void write_top(const ProbsArgs &a, int64_t r, int j, float v, int32_t id, float lse) {
-  const float z = v * a.scale;
+// what a row's statistics say, written by one lane
+__device__ __forceinline__ void finish_row(const ProbsArgs &a, int64_t r, float m, float s, float u, float log_s, float target, bool has) {
+  const bool none = s == 0.f;
+  if (a.lse) {                               // one of finite logits is finite: the largest number where it passes the range
+    const float lse = m * a.scale + log_s;
+    a.lse[r] = none || lse != lse ? lse : __builtin_amdgcn_fmed3f(lse, -__FLT_MAX__, __FLT_MAX__);
+  }
+  if (a.entropy) a.entropy[r] = none ? 0.f : log_s - u * kLn2 / s;
+  if (a.logp) a.logp[r] = has ? log_p(target, m, log_s, a.scale) : 0.f;
+}
+__device__ __forceinline__ void write_top(const ProbsArgs &a, int64_t r, int j, float v, int32_t id, float m, float log_s) {
   if (a.top_ids) a.top_ids[r * a.top + j] = id;
-  if (a.top_logp) a.top_logp[r * a.top + j] = lse == -__builtin_inff() ? lse : z - lse;
+  if (a.top_logp) a.top_logp[r * a.top + j] = log_p(v, m, log_s, a.scale);
 }
 
 // ------------------------------------------------------------------------------------ short rows
@@ -160,7 +167,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_rows(ProbsArgs a) {
     for (int i = 0; i < NV; i++) load_pack<T, V>(x + min((i * L + q) * V, C - V), f[i]);
     const int64_t t = target_of(a.targets, a.wide_targets, r);
     const bool has = t >= 0 && t < C;
-    const float zt = has ? (float)x[t] * a.scale : 0.f;
+    const float target = has ? (float)x[t] : 0.f;
     uint32_t list[KL > 0 ? KL : 1];
 #pragma unroll
     for (int k = 0; k < KL; k++) list[k] = 0;
@@ -192,8 +199,8 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_rows(ProbsArgs a) {
     s = group_sum<L>(s);
     u = group_sum<L>(u);
     const bool on = mine < a.rows;
-    const float lse = row_lse(m, s, a.scale);
-    if (on && q == 0) finish_row(a, r, s, u, lse, zt, has);
+    const float log_s = logf(s);
+    if (on && q == 0) finish_row(a, r, m, s, u, log_s, target, has);
     if constexpr (K > 0) {
       uint32_t o[KL];
       bool open = s != s;                    // a NaN (or +inf) in the row
@@ -234,7 +241,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_rows(ProbsArgs a) {
       }
 #pragma unroll
       for (int i = 0; i * L < K; i++)
-        if (on && i * L + q < a.top) write_top(a, r, i * L + q, v[i], id[i], lse);
+        if (on && i * L + q < a.top) write_top(a, r, i * L + q, v[i], id[i], m, log_s);
     }
   }
 }
@@ -377,11 +384,11 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
         a.part_id[p * a.top + threadIdx.x] = s_id[W * KS + threadIdx.x];
       }
     } else {
-      const float lse = row_lse(safe_max(bm), s, a.scale);
+      const float m = safe_max(bm), log_s = logf(s);
       if (tid == 0) {
         const int64_t t = target_of(a.targets, a.wide_targets, r);
         const bool has = t >= 0 && t < a.classes;
-        finish_row(a, r, s, u, lse, has ? (float)x[t] * a.scale : 0.f, has);
+        finish_row(a, r, m, s, u, log_s, has ? (float)x[t] : 0.f, has);
       }
       if constexpr (K > 0) {
         uint32_t o = 0;
@@ -396,7 +403,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_long(ProbsArgs a) {
             if (tid == k) { o = oo; id = ii; }
           }
         }
-        if (tid < a.top) write_top(a, r, tid, of_order(o), id, lse);
+        if (tid < a.top) write_top(a, r, tid, of_order(o), id, m, log_s);
       }
     }
     if constexpr (TW > kWave) __syncthreads();               // LDS is the next row's
@@ -414,12 +421,12 @@ __global__ __launch_bounds__(kWave) void k_probs_join(ProbsArgs a) {
     const float m = safe_max(group_all<kWave>(st.m, [](float x, float y) { return fmaxf(x, y); }));
     rescale(st, m, a.scale * kLog2e);
     const float s = group_sum<kWave>(st.s), u = group_sum<kWave>(st.u);
-    const float lse = row_lse(m, s, a.scale);
+    const float log_s = logf(s);
     if (l == 0) {
       const T *x = static_cast<const T *>(a.logits) + r * a.ld;
       const int64_t t = target_of(a.targets, a.wide_targets, r);
       const bool has = t >= 0 && t < a.classes;
-      finish_row(a, r, s, u, lse, has ? (float)x[t] * a.scale : 0.f, has);
+      finish_row(a, r, m, s, u, log_s, has ? (float)x[t] : 0.f, has);
     }
     if constexpr (K > 0) {
       Best<float, K> b;
@@ -435,7 +442,7 @@ __global__ __launch_bounds__(kWave) void k_probs_join(ProbsArgs a) {
         take_best<kWave, K>(b, o, id);
         if (l == k) { my_o = o; my_id = id; }
       }
-      if (l < a.top) write_top(a, r, l, of_order(my_o), my_id, lse);
+      if (l < a.top) write_top(a, r, l, of_order(my_o), my_id, m, log_s);
     }
   }
 }
