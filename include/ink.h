@@ -423,7 +423,8 @@ ink_status ink_log_probs(const void *logits, int64_t ld, const void *targets, in
 
 /* Gradient of sum_r g_logp[r] logp[r] + g_entropy[r] entropy[r] by the logits, [rows][classes] of `type` (not that of lse or
  * top_logp).  Either of g_logp and g_entropy may be NULL; lse and entropy as the forward call wrote them (entropy
- * is read with g_entropy only).  A row without a target takes no part in g_logp; a row of masked classes has gradient 0. */
+ * is read with g_entropy only).  A row without a target takes no part in g_logp; a row of masked classes has gradient 0.
+ * Where lse lies beyond -256 .. 256 the row's sum is formed anew: a float near that size does not hold log p. */
 ink_status ink_log_probs_backward(const void *logits, int64_t ld, const void *targets, int32_t target_bytes, const float *lse,
                                   const float *entropy, const float *g_logp, const float *g_entropy, int64_t rows, int64_t classes,
                                   int32_t type, float scale, void *dlogits, int64_t ld_out, void *hip_stream);

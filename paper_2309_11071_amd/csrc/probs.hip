@@ -5,7 +5,7 @@
 //   gradient of g log p_t + h entropy:  scale (g ([c = t] - p_c) - h p_c (log p_c + entropy))
 //
 // log p is a difference of logits and log S: formed of those it has the same digits wherever a row lies, which z - lse has near zero only
-// (47 logits near 20000: 1.2e-7 off, and 8.7e-4).  S, not lse, says whether a row has a class left.
+// (47 logits near 20000: 1.0e-6 off, and 9.8e-4).  S, not lse, says whether a row has a class left.
 //
 // The alternatives are the classes of the largest logits, compared as they stand in memory: equal ones by the lower class, NaN
 // before everything, -0 equal to +0.  A class at -inf is masked (p = 0); a row of masked classes has lse = log p = -inf, entropy
@@ -23,7 +23,7 @@
 // has NaN, the row is done again by full comparisons.  In long rows a wave skips what is below K values it has seen.
 //
 // 2.45M x 47 bf16: without alternatives 56 us (4.9 TB/s), with 5 99 (vector instructions, some 700 for 32 rows); 512 x 100003 f16 29 and, with 8,
-// 46; the gradient of 1M x 172 f32 270 (5.2 TB/s).
+// 46; the gradient of 1M x 172 f32 235 (6.0 TB/s), 340 where every row is far from zero.
 #include <algorithm>
 
 #include "head.h"
@@ -457,6 +457,53 @@ struct ProbsGradArgs {
   float scale;
 };
 
+// Beyond this lse of 32 bits is off by more than 1.5e-5, and so would be every p that is formed with it; at a type's lowest values
+// it holds nothing of log S at all.
+constexpr float kFarLse = 256.f;
+
+// The gradient by one logit, from its class's log probability.  p comes in two factors: the hardware's exponential knows no subnormal
+// results, which 32-bit and bf16 gradients have.
+struct GradTerm {
+  float g, h, ent, scale;                    // gradients of log p_t and entropy, 0 where there are none
+  __device__ __forceinline__ float operator()(float lp, bool target) const {
+    const float root = __builtin_amdgcn_exp2f(lp * (0.5f * kLog2e));
+    return (root * (-g - h * (fmaxf(lp, -1e30f) + ent)) * root + (target ? g : 0.f)) * scale;
+  }
+};
+
+// A row far from zero, by one group of lanes: maximum and sum anew, then its gradient.  Three reads instead of one.
+template <class T, int L, int V> __device__ __forceinline__ void far_row(const ProbsGradArgs &a, const T *x, T *out, int64_t t, GradTerm term) {
+  const int q = threadIdx.x % L;
+  const float scale2 = a.scale * kLog2e;
+  float m = -__builtin_inff(), s = 0.f;
+#pragma unroll 1
+  for (int64_t first = q * V; first < a.classes; first += L * V) {
+    float f[V];
+    load_pack<T, V>(x + min(first, a.classes - V), f);
+#pragma unroll
+    for (int j = 0; j < V; j++) m = fmaxf(m, f[j]);
+  }
+  m = safe_max(group_all<L>(m, [](float p, float p2) { return fmaxf(p, p2); }));
+#pragma unroll 1
+  for (int64_t first = q * V; first < a.classes; first += L * V) {
+    const int64_t at = min(first, a.classes - V);
+    float f[V];
+    load_pack<T, V>(x + at, f);
+#pragma unroll
+    for (int j = 0; j < V; j++) s += at + j >= first ? __builtin_amdgcn_exp2f((f[j] - m) * scale2) : 0.f;
+  }
+  const float log_s = logf(group_sum<L>(s));
+#pragma unroll 1
+  for (int64_t first = q * V; first < a.classes; first += L * V) {
+    const int64_t at = min(first, a.classes - V);
+    float f[V];
+    load_pack<T, V>(x + at, f);
+#pragma unroll
+    for (int j = 0; j < V; j++) f[j] = term(log_p(f[j], m, log_s, a.scale), at + j == t);
+    store_pack<T, V>(out + at, f);
+  }
+}
+
 template <class T, int L, int NV, int V>
 __global__ __launch_bounds__(kHeadThreads) void k_probs_grad(ProbsGradArgs a) {
   constexpr int G = kHeadThreads / L;
@@ -471,23 +518,24 @@ __global__ __launch_bounds__(kHeadThreads) void k_probs_grad(ProbsGradArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; i++) load_pack<T, V>(x + min(c0 + (i * L + q) * V, a.classes - V), z[i]);
     const int64_t t = target_of(a.targets, a.wide_targets, r);
-    float lse = a.lse[r];
+    float lse = a.lse[r], g = a.g_logp ? a.g_logp[r] : 0.f, h = 0.f, ent = 0.f;
+    if (a.g_entropy) { h = a.g_entropy[r]; ent = a.entropy[r]; }
     const bool none = lse == -__builtin_inff();            // every class masked: no gradient
     lse = none ? 0.f : lse;
-    const float g = a.g_logp && t >= 0 && t < a.classes && !none ? a.g_logp[r] : 0.f;
-    const float h = a.g_entropy && !none ? a.g_entropy[r] : 0.f, ent = a.g_entropy ? a.entropy[r] : 0.f;
+    h = none ? 0.f : h;
+    g = none || t < 0 || t >= a.classes ? 0.f : g;
+    const GradTerm term = {g, h, ent, a.scale};
+    const bool far = fabsf(lse) > kFarLse;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       const int64_t first = c0 + (i * L + q) * V, at = min(first, a.classes - V);
       float o[V];
 #pragma unroll
-      for (int j = 0; j < V; j++) {
-        const float lp = z[i][j] * a.scale - lse, p = __builtin_amdgcn_exp2f(lp * kLog2e);
-        const float d = p * (-g - h * (fmaxf(lp, -1e30f) + ent)) + (at + j == t ? g : 0.f);
-        o[j] = d * a.scale;
-      }
-      if (first < a.classes) store_pack<T, V>(out + at, o);
+      for (int j = 0; j < V; j++) o[j] = term(z[i][j] * a.scale - lse, at + j == t);
+      if (first < a.classes && !far) store_pack<T, V>(out + at, o);
     }
+    // rare; a group's lanes agree, and of a row in pieces the first one's group does all
+    if (far && c0 == 0) far_row<T, L, V>(a, x, out, t, term);
   }
 }
 
