@@ -462,12 +462,12 @@ struct ProbsGradArgs {
 constexpr float kFarLse = 256.f;
 
 // The gradient by one logit, from its class's log probability.  p comes in two factors: the hardware's exponential knows no subnormal
-// results, which 32-bit and bf16 gradients have.
+// results, which 32-bit and bf16 gradients have.  Below log p = -200 both factors are zero, and what they multiply has to be finite.
 struct GradTerm {
   float g, h, ent, scale;                    // gradients of log p_t and entropy, 0 where there are none
   __device__ __forceinline__ float operator()(float lp, bool target) const {
     const float root = __builtin_amdgcn_exp2f(lp * (0.5f * kLog2e));
-    return (root * (-g - h * (fmaxf(lp, -1e30f) + ent)) * root + (target ? g : 0.f)) * scale;
+    return (root * (-g - h * (fmaxf(lp, -200.f) + ent)) * root + (target ? g : 0.f)) * scale;
   }
 };
 

@@ -68,3 +68,18 @@ def test_gradient_of_rows_at_the_ends_of_a_type(rows, classes, dtype):
         equal[1], equal[2] = True, False
         close(got[equal], want[equal], tol, dtype, "rows of equal logits")
         assert (got[~equal] == 0).all(), "one class left, or none"
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("classes", [7, 300, 5003])
+def test_large_gradients_of_masked_classes(dtype, classes):
+    """p = 0 and log p = -inf: such a class takes no part in the entropy, whatever the entropy's gradient is."""
+    x = torch.zeros(3, classes).to(dtype)
+    x[:, 2:] = -float("inf")
+    x[2] -= 1000
+    out = head.log_probs(x.cuda(), None)
+    h = torch.full((3,), 1e9).cuda()
+    got = head.log_probs_backward(x.cuda(), None, out["lse"], out["entropy"], g_entropy=h).double().cpu()
+    assert (got[:, 2:] == 0).all()
+    # -h p (log p + H): zero but for the errors of log p, H and lse, each of a few u (lse of the third row is formed anew)
+    assert got[:, :2].abs().max() <= 1e9 * 0.5 * 16 * u
