@@ -3,7 +3,8 @@ each with its gradient (include/ink.h has what they compute).
 
 Argument marshalling only: every operator runs inside libink.so.  Calls are asynchronous on torch's
 current stream of the tensors' device, like torch's own; results and work memory come from torch's
-allocator.  Nothing is recorded for autograd: the gradients are calls of their own.  A matrix is a 2-D
+allocator.  Nothing is recorded for autograd: the gradients are calls of their own, and a tensor that requires a
+gradient raises unless it is detached or the call stands under torch.no_grad().  A matrix is a 2-D
 tensor whose rows are contiguous, at any distance from each other; any other layout is copied first.
 Tensors of other devices or types and shapes that do not fit raise.
 """
@@ -42,6 +43,13 @@ def _functions():
     return _fn
 
 
+def _unrecorded(t, name):
+    """Raises where autograd would expect a record of the call; t requires a gradient."""
+    if torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, and these operators record nothing for autograd: detach it or call under torch.no_grad(), "
+                         "and use the *_backward calls" % name)
+
+
 def _matrix(t, name, rows=None, cols=None, dtype=None, like=None):
     """t as a matrix of contiguous rows on a GPU, and the distance of its rows; raises where it is none or not of this
     shape, type and device."""
@@ -54,6 +62,8 @@ def _matrix(t, name, rows=None, cols=None, dtype=None, like=None):
         raise ValueError("%s has shape %s, wanted [%s, %s]" % (name, tuple(t.shape), "rows" if rows is None else rows, m if cols is None else cols))
     if like is not None and t.device != like.device:
         raise ValueError("%s is on %s, the rows on %s" % (name, t.device, like.device))
+    if t.requires_grad:
+        _unrecorded(t, name)
     s0, s1 = t.stride()
     if (s1 != 1 and m > 1) or (s0 < m and s0 != 0 and n > 1):
         t = t.contiguous()
@@ -69,6 +79,8 @@ def _vector(t, name, n, like, dtypes):
         raise ValueError("%s must be a GPU tensor of shape [%d] on the rows' device" % (name, n))
     if t.dtype not in dtypes:
         raise TypeError("%s has type %s, wanted %s" % (name, t.dtype, " or ".join(str(d) for d in dtypes)))
+    if t.requires_grad:
+        _unrecorded(t, name)
     return t if n < 2 or t.stride(0) == 1 else t.contiguous()
 
 
