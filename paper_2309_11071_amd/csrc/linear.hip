@@ -7,7 +7,7 @@
 // reading the rows and writing the results, 32-bit ones by the matrix unit.  Every product is formed transposed, W's columns as
 // the instruction's rows, so that a lane ends up with four neighbouring columns of its row.  Which kernel:
 //
-//   up to 64 rows               k_linear_few     a row and 32 columns a workgroup; W is what is read: 1 x 602 x 256 bf16 5 us
+//   up to 64 rows, 64k results  k_linear_few     a row and 32 columns a workgroup; W is what is read: 1 x 602 x 256 bf16 5 us
 //   from 32768 rows on          k_linear_stream  W in registers, rows in a stream; up to 640 terms (16 bits) or 256 (32 bits)
 //   enough rows for 256 tiles   k_linear_tile    128 rows by 64 or 128 columns
 //   else                        k_linear_small   32 by 32, eight waves share the depth: 100 x 602 x 256 f32 37 us in tiles, 11 (the call) so
@@ -925,8 +925,11 @@ __global__ __launch_bounds__(256) void k_grad_sum(GradSumArgs a) {
 }
 
 // ------------------------------------------------------------------------------------ host side
-constexpr int64_t kFewRows = 64;             // rows that workgroups take one by one, W from the caches for each: bf16, 1 / 16 / 32 rows of
-                                             // 602 x 256 5.2 / 4.9 / 5.0 us, k_linear_small 8.4 / 8.4 / 8.5; 32 of 1024 x 1024 6.8 and 12.5
+// Rows that workgroups take one by one (k_linear_few), each asking for all of W.  Both kernels' time goes with the depth; what is asked for again comes on
+// top, so the limit is on rows times columns.  us a call, k_linear_few and k_linear_small: bf16 4096 x 4096 16 rows (at the limit) 35 and 76, 32 rows 83
+// and 77; 16384 x 16384 4 rows 391 and 492, 8 rows 913 and 491, 64 rows 9720 and 536; 256 x 16384 4 rows 8.7 and 8.6, 64 rows 54 and 10; 16384 x 256
+// 64 rows 91 and 331; f32 4096 x 4096 16 rows 42 and 46, 32 rows 86 and 50; 16384 x 16384 4 rows 296 and 316, 8 rows 719 and 318.
+constexpr int64_t kFewRows = 64, kFewResults = 64 * 1024;
 constexpr int64_t kStreamRows = 32 * 1024;   // rows from which on a workgroup that lays out W for itself takes several tiles
 template <class T, class TI, class TO, int KS, int NTW, int WN, int WM, int WK, int PER, bool GRAD>
 static void stream_launch(const LinearArgs &a, Launches &run) {
@@ -980,7 +983,7 @@ template <class T, class TI, class TO, bool GRAD> static bool stream_run(const L
 
 template <class T, class TI, class TO, bool GRAD> static void linear_run(const LinearArgs &a, Launches &run) {
   if constexpr (!GRAD)
-    if (a.rows <= kFewRows) return run(k_linear_few<T, TO>, dim3((a.width + 31) / 32, (unsigned)a.rows), dim3(kHeadThreads), a);
+    if (a.rows <= kFewRows && a.rows * a.width <= kFewResults) return run(k_linear_few<T, TO>, dim3((a.width + 31) / 32, (unsigned)a.rows), dim3(kHeadThreads), a);
   if (stream_run<T, TI, TO, GRAD>(a, run)) return;
   const int64_t tiles = (a.rows + 127) / 128;
   const int ntw = a.width <= 64 ? 1 : 2, gy = (a.width + 64 * ntw - 1) / (64 * ntw);

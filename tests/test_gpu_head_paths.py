@@ -53,6 +53,18 @@ def test_linear_in_tiles(rows, cols, out, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,out", [(64, 300, 1024), (64, 300, 1025), (4, 200, 16384), (5, 200, 16384), (2, 4100, 4100), (61, 1030, 5000)])
+def test_linear_of_few_rows_and_wide_results(rows, cols, out, dtype):
+    """Beside the number of results up to which rows are taken one by one, and far beyond it."""
+    g, x, w, b = linear_case(rows, cols, out, dtype, rows + cols + out)
+    r = torch.randn(rows, out, generator=g).to(dtype)
+    y, z = head.linear(table(x, cols + 1, 1), table(w, out + 3, 1), b.cuda(), act="silu", residual=table(r, out + 1, 1), keep_pre=True)
+    want = linear_ref(x, w, b, "silu", r)
+    close(z, want[1], want[3], dtype, "z")
+    close(y, want[0], want[2], dtype, "y")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,out", [(20_000, 256, 256), (32_700, 48, 700), (8_200, 513, 511)])
 def test_linear_backward_in_tiles(rows, cols, out, dtype):
     g, x, w, _ = linear_case(rows, cols, out, dtype, rows * 3 + cols + out)
