@@ -52,8 +52,8 @@ extern "C" {
 #define INK_MAX_OUT_DIM 256
 #define INK_MAX_IN_DIM 16384
 #define INK_MAX_LAYERS 8
-#define INK_MAX_CLASSES (1 << 27) /* ink_log_probs: classes of a row, and alternatives asked for */
-#define INK_MAX_TOP 16
+#define INK_MAX_CLASSES (1 << 27) /* ink_log_probs: classes of a row */
+#define INK_MAX_TOP 16            /* ink_log_probs: alternatives asked for */
 
 typedef struct ink_ctx ink_ctx; /* opaque; owns all device state */
 

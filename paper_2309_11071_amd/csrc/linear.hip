@@ -16,8 +16,10 @@
 // which the matrix unit holds up, 50k rows 19 and 19, 200k 49 and 54.
 //
 // Products are exact (16-bit operands) or fused (32 bits), and summed in 32 bits; the epilogue is in 32 bits and y, z, dx, dweight and
-// dbias are rounded once.  For 16-bit rows dz is rounded to the rows' type before the two products, which take 16-bit operands: an error
-// of the size of the results' own rounding, for half the matrix instructions of two 16-bit parts; dbias sums the unrounded values.  dweight is
+// dbias are rounded once.  For 16-bit rows dz is rounded to the rows' type before the two products, as a program that keeps dz in memory
+// has it: an error of the size of the results' own rounding (612k x 128 x 172 bf16 with gelu 0.0024 from 64 bits, 0.0017 rounded once).  dz in two
+// 16-bit parts gives results rounded once; the second part's conversions, its room in LDS and its matrix instructions cost 612k x 128 x 172 242 us instead of
+// 194, 128 x 47 113 instead of 110, 256 x 256, whose registers it does not fit, 1016 instead of 556.  dbias sums the unrounded values.  dweight is
 // a sum over all rows: workgroups take slices of the rows and leave a partial matrix each, which k_grad_sum adds up in order (no
 // atomics: the same call gives the same bits).
 #include <algorithm>
@@ -230,8 +232,8 @@ template <class T, class TI, bool GRAD> __device__ __forceinline__ typename Frag
 // T: type of the operands, TI: of the rows read (GRAD: dy and z), TO: of the rows written.
 // 128 rows by 64 NTW columns a workgroup, 64 by 32 NTW a wave, 128 bytes of the depth in LDS at a time: while one piece is
 // multiplied the next is on its way in registers.  For 32-bit rows, which the matrix unit bounds, and depths whose W the registers of a
-// workgroup do not hold.  One buffer and three workgroups a CU against two buffers (one barrier a piece) and two workgroups: 233k x 602 x 256
-// f32 782 and 815 us; tiles of 64 rows and four workgroups 789.
+// workgroup do not hold.  233k x 602 x 256 f32 takes 655 us (110 TFLOP/s).  One buffer and three workgroups a CU against two buffers (one barrier a
+// piece) and two workgroups, both before products of different accumulators took turns: 782 and 815 us; tiles of 64 rows and four workgroups 789.
 template <class T, class TI, class TO, int NTW, bool GRAD>
 __global__ __launch_bounds__(256, 3) void k_linear_tile(LinearArgs a) {
   typedef typename Frag<T>::V V;
@@ -391,9 +393,10 @@ __global__ __launch_bounds__(kWave * kSmallWaves) void k_linear_small(LinearArgs
 // ahead, and put them into LDS, from where every wave reads the fragments of its 32 rows; the product goes through
 // LDS in 32 bits once more, so that residual, z and y are read and written in whole lines too.  Bound by memory in 16 bits: 2.45M x 256 x
 // 256 with residual and z 1.0 ms (5.02 GB, 4.9 TB/s), without 0.59 (4.2), 2.45M x 128 x 64 167 us (5.6); the matrix unit is busy 15 % of the time.  In
-// 32 bits the matrix unit and memory take turns: 2.45M x 128 x 64 475 us, 85 TFLOP/s.  The group sizes are those that
-// leave the registers without spills (256 with two waves a SIMD) and were the fastest of those measured: 602 x 256 with a 20-step half
-// of the depth a wave 541 us, with all 40 steps of 32 columns 425; 602 x 47 split four ways 214, unsplit 363.
+// 32 bits the matrix unit and memory take turns: 2.45M x 128 x 64 460 us, 87 TFLOP/s.  The group sizes are the fastest of those
+// measured: 612k x 602 x 256 bf16 with all 40 steps of 32 columns a wave 473 us, with 20-step halves and 64 columns a wave 672, with halves over sixteen
+// waves 622; 612k x 602 x 47 split four ways 174, unsplit 639.  Not all fit the registers (256 with two waves a SIMD, 128 with four): the
+// forms of 40 steps spill 37 to 94, those of 8 steps a wave at four waves a SIMD 6 to 12 in the gradient, 93 there with 32-bit rows.
 struct StreamArgs {
   LinearArgs a;
   int chunks, pitch, flat;                   // 16-byte pieces of a row's depth; floats between rows of results in LDS; see emit
@@ -646,7 +649,8 @@ __global__ __launch_bounds__(kHeadThreads) void k_linear_few(LinearArgs a) {
 // A workgroup has the sums of 32 KT columns of x by 32 NT of dz in registers, (KT / 2) (NT / 2) tiles a wave, and takes 32 rows at a time
 // (64 with eight waves, which larger tiles take), one piece ahead in registers.  All threads load x, dy and z side by side, 16 bytes a lane, form dz once and put both into LDS row by row.  The
 // sums run over the rows, so their fragments are columns: 16-bit ones come from the transposing LDS read, 32-bit ones element by
-// element.  The partial sums are left in the fragments' order and k_grad_sum puts them where they belong.
+// element.  The partial sums are left in the fragments' order and k_grad_sum puts them where they belong.  dbias without dweight takes the
+// same kernel, whose products are then of zeros.
 // 612k x 128 x 172 bf16: without an activation 142 us (3.7 TB/s of the bytes it cannot do without), with gelu 198: the slope is formed once an
 // element, and its 25 instructions are what bounds that.
 struct GradArgs {
@@ -656,7 +660,6 @@ struct GradArgs {
   int64_t rows, ld_x, ld_dy, ld_pre, ld_w, ld_dx, slice;
   int cols, out, act;
 };
-constexpr int kGradRows = 32;                // rows that a slice is a multiple of
 
 // Bytes between rows in LDS: rows of 16 lanes' pieces fall on all banks, and in 32 bits two rows side by side nearly so.
 template <class T, int TILES> constexpr int kGradPitch = TILES * 32 * (int)sizeof(T) + (sizeof(T) == 2 ? 16 : 144);
@@ -859,8 +862,8 @@ __global__ __launch_bounds__(kWave * WAVES, 2) void k_linear_grad(GradArgs a) {
         }
   }
   if (!a.part_bias || blockIdx.x) return;
-  // column sums of dz: each thread's of its row's pieces, over the 32 rows.  A moved piece's first columns belong to the one before.
-  float *s_sum = DB_LDS ? s_db : reinterpret_cast<float *>(s_mem);           // [32][PB]
+  // column sums of dz: each thread's of its row's pieces, over the ROWS rows.  A moved piece's first columns belong to the one before.
+  float *s_sum = DB_LDS ? s_db : reinterpret_cast<float *>(s_mem);           // [ROWS][PB]
   float own[NZ][VK];
 #pragma unroll
   for (int j = 0; j < NZ; j++)

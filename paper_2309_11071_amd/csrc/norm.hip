@@ -4,8 +4,8 @@
 //   gradient  h = (x - mean) rstd,  g = dy weight:   dx = rstd (g - mean(g) - h mean(g h)),
 //             dweight = sum over rows of dy h,  dbias = sum over rows of dy
 //
-// Both are bound by memory, eight to eleven operations an element against 4 to 12 bytes, and run at the rate of a copy (5.0 TB/s):
-// 2.45M x 256 bf16 forward 504 us, 233k x 602 f32 gradient 340 us, 5 of them for the partial rows' sum.  So a row is read once: L lanes hold it
+// Both are bound by memory, eight to eleven operations an element against 4 to 12 bytes, and run at the rate of a copy (5.0 TB/s)
+// where a wave holds a row: 2.45M x 256 bf16 forward 504 us, 233k x 602 f32 gradient 332 us, 5 of them for the partial rows' sum.  So a row is read once: L lanes hold it
 // in registers, V elements (16 bytes) a load and NV loads a lane, and the variance is taken of the differences from the mean
 // without a second read.  L is the smallest group that holds a row with NV <= 4: the fewer lanes a row has, the fewer steps
 // its sums take and the more rows a wave has under way.  The last load of a row that is no multiple of V elements starts V
@@ -15,6 +15,10 @@
 // The weights' gradient is a sum over all rows: a lane keeps those of its columns in registers over all rows that its workgroup
 // takes, the workgroup adds up its groups in LDS and leaves one partial row, and k_norm_params adds the partial
 // rows in their order.  No atomics: the same call gives the same bits.
+//
+// Rows that a wave does not hold (f32 from 1025 columns on, 16 bits from 2049) have a workgroup of 1024 threads each, which little more than that
+// leaves idle: f32 200k x 1100 takes 2.4 times a copy's time forward and 2.8 in the gradient, 100k x 2048 1.3 and 1.7, 50k x 4096 0.9 and 1.1, 20k x 8192
+// 0.9 and 0.9; bf16 100k x 2100 3.0 and 2.7, 50k x 4096 1.6 and 1.5, 20k x 16384 1.0 and 1.0.
 #include <algorithm>
 
 #include "head.h"

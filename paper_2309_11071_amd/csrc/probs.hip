@@ -20,7 +20,9 @@
 // of all lists, once per alternative.  An element is one number, its order above its class, so that a place of the list costs one
 // instruction (the median of the place, the one above and the element).  16-bit logits and their classes fit into 32 bits; of 32-bit logits
 // the lowest bits give way to the class, and where that leaves the order open (equal upper bits at the list's end or within it), or a row
-// has NaN, the row is done again by full comparisons.  In long rows a wave skips what is below K values it has seen.
+// has NaN, its wave's rows are done again by full comparisons.  In long rows a wave skips what is below K values it has seen.
+// Equal upper bits are rare among continuous 32-bit logits, not among rounded ones: 1M x 172 f32 with 5 alternatives takes 214 us, of logits that were
+// bf16 342, f16 236, of relu's zeros where few classes are above them 399 (2.45M x 47 148, 261, 182, 272).
 //
 // 2.45M x 47 bf16: without alternatives 56 us (4.9 TB/s), with 5 99 (vector instructions, some 700 for 32 rows); 512 x 100003 f16 29 and, with 8,
 // 46; the gradient of 1M x 172 f32 235 (6.0 TB/s), 340 where every row is far from zero.
