@@ -232,7 +232,7 @@ template <class T, class TI, bool GRAD> __device__ __forceinline__ typename Frag
 // T: type of the operands, TI: of the rows read (GRAD: dy and z), TO: of the rows written.
 // 128 rows by 64 NTW columns a workgroup, 64 by 32 NTW a wave, 128 bytes of the depth in LDS at a time: while one piece is
 // multiplied the next is on its way in registers.  For 32-bit rows, which the matrix unit bounds, and depths whose W the registers of a
-// workgroup do not hold.  233k x 602 x 256 f32 takes 655 us (110 TFLOP/s).  One buffer and three workgroups a CU against two buffers (one barrier a
+// workgroup do not hold.  233k x 602 x 256 f32 takes 674 us (106 TFLOP/s).  One buffer and three workgroups a CU against two buffers (one barrier a
 // piece) and two workgroups, both before products of different accumulators took turns: 782 and 815 us; tiles of 64 rows and four workgroups 789.
 template <class T, class TI, class TO, int NTW, bool GRAD>
 __global__ __launch_bounds__(256, 3) void k_linear_tile(LinearArgs a) {

@@ -41,3 +41,12 @@ def test_the_widest_rows(lib):
     assert linear(MAX_COLS, MAX_COLS) == 0 and linear(MAX_COLS + 1, 8) == 1 and linear(8, MAX_COLS + 1) == 1
     assert lib.ink_linear_backward_work(1, MAX_COLS, MAX_COLS) > 0 and lib.ink_linear_backward_work(1, MAX_COLS + 1, 8) == 0
     assert lib.ink_layer_norm_backward_work(MAX_ROWS, MAX_COLS, 0) > 0 and lib.ink_layer_norm_backward_work(MAX_ROWS + 1, 8, 0) == 0
+
+
+def test_the_largest_scale(lib):
+    """The scale's product with log2 e has to be a number."""
+    def call(scale):
+        return (lib.ink_log_probs(None, 8, None, 0, 0, 8, 0, scale, 0, None, None, None, None, None, None, 0, None),
+                lib.ink_log_probs_backward(None, 8, None, 0, None, None, None, None, 0, 8, 0, scale, None, 8, None))
+    assert call(2.3e38) == (0, 0)
+    assert call(2.4e38) == (1, 1) and "scale" in lib.ink_last_error(None).decode()
