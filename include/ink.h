@@ -415,7 +415,7 @@ ink_status ink_linear_backward(const void *dy, int64_t ld_dy, const void *x, int
  * logits are numbers like others, a type's lowest among them, but for one further below its row's largest than a float can
  * say (masked).  log p is formed of differences of logits and has its digits however far from zero these lie; where lse passes
  * the range of float it is the largest finite number of its sign.
- *   scale     > 0 (1 / temperature);  classes 1 .. INK_MAX_CLASSES */
+ *   scale     > 0, at most 2.3e38 (1 / temperature);  classes 1 .. INK_MAX_CLASSES */
 size_t ink_log_probs_work(int64_t rows, int64_t classes, int32_t type, int32_t top);
 ink_status ink_log_probs(const void *logits, int64_t ld, const void *targets, int32_t target_bytes, int64_t rows, int64_t classes,
                          int32_t type, float scale, int32_t top, float *logp, float *entropy, float *lse, int32_t *top_ids,

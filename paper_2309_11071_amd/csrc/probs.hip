@@ -643,7 +643,7 @@ static const char *probs_check(const void *targets, int32_t target_bytes, int64_
   if (!known_type(type)) return "unknown type";
   if (rows < 0 || rows > kMaxHeadRows) return "rows out of range";
   if (classes < 1 || classes > INK_MAX_CLASSES) return "classes must be 1 .. INK_MAX_CLASSES";
-  if (!(scale > 0.f) || scale > 3e38f) return "scale must be positive and finite";
+  if (!(scale > 0.f) || scale > 2.3e38f) return "scale must be positive and at most 2.3e38";       // scale log2 e is a number
   if (targets && target_bytes != 4 && target_bytes != 8) return "target_bytes must be 4 or 8";
   if (targets && !aligned_to(targets, target_bytes)) return "targets are not aligned";
   return nullptr;
