@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2309_11071_amd import head
-from test_gpu_head import F32, TYPES, close, gen, table, u
+from test_gpu_head import TYPES, close, gen, table, u
 from test_gpu_head_logits import SHAPES, exact, far_rows
 
 pytestmark = pytest.mark.gpu
