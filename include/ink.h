@@ -54,6 +54,7 @@ extern "C" {
 #define INK_MAX_LAYERS 8
 #define INK_MAX_CLASSES (1 << 27) /* ink_log_probs: classes of a row */
 #define INK_MAX_TOP 16            /* ink_log_probs: alternatives asked for */
+#define INK_ADAMW_BLOCK 128       /* ink_adamw: neighbouring elements whose 8-bit moments share a scale */
 
 typedef struct ink_ctx ink_ctx; /* opaque; owns all device state */
 
@@ -80,7 +81,9 @@ typedef enum {
 /* GELU (z times the normal distribution function) and SILU (z times the logistic function): ink_linear only,
  * a layer takes NONE or RELU. */
 typedef enum { INK_ACT_NONE = 0, INK_ACT_RELU = 1, INK_ACT_GELU = 2, INK_ACT_SILU = 3 } ink_act;
-typedef enum { INK_F32 = 0, INK_BF16 = 1, INK_F16 = 2 } ink_type; /* element types of an answer head's operators */
+typedef enum { INK_F32 = 0, INK_BF16 = 1, INK_F16 = 2, /* element types of an answer head's operators */
+               INK_E4M3 = 3, /* 8 bits (4 of exponent, 3 of mantissa, largest number 448), where an operator says so */
+               INK_NO_TYPE = -1 } ink_type;
 typedef enum { INK_MEM_HOST = 0, INK_MEM_DEVICE = 1 } ink_mem;
 
 /* In-neighbour CSR of the initial snapshot: row v lists the sources u of edges u -> v,
@@ -428,6 +431,74 @@ ink_status ink_log_probs(const void *logits, int64_t ld, const void *targets, in
 ink_status ink_log_probs_backward(const void *logits, int64_t ld, const void *targets, int32_t target_bytes, const float *lse,
                                   const float *entropy, const float *g_logp, const float *g_entropy, int64_t rows, int64_t classes,
                                   int32_t type, float scale, void *dlogits, int64_t ld_out, void *hip_stream);
+
+/* Root-mean-square norm of rows after the addition of a residual: t = x + residual, rounded to `type`;
+ * y = t * rstd * weight, rstd = 1 / sqrt(mean of t^2 + eps).
+ *   x, residual  [rows][cols] of `type`; residual NULL: t is x
+ *   weight       [cols] of `param_type` (`type` or INK_F32), or NULL: 1
+ *   y            [rows][cols] of `out_type`, `type` or INK_E4M3: then scale[r] = max |y| of the row / 448 and y holds the numbers y / scale, each
+ *                rounded to nearest even.  A row whose largest |y| is below 448 * 2^-126 has scale 0 and zeros, one with a NaN or an
+ *                infinity scale and codes NaN
+ *   total        [rows][cols] of `type`, gets t where residual is not NULL (for the next block and the gradient)
+ *   rstd         [rows] float, written for the gradient, or NULL;  scale [rows] float, for INK_E4M3 only
+ *   eps          > 0
+ * The squares are summed in 32 bits: a row whose sum passes their range (elements beyond 10^19) has rstd 0. */
+ink_status ink_rms_norm(const void *x, int64_t ld_x, const void *residual, int64_t ld_res, const void *weight, int64_t rows, int32_t cols,
+                        int32_t type, int32_t param_type, float eps, int32_t out_type, void *y, int64_t ld_y, float *scale, void *total,
+                        int64_t ld_total, float *rstd, void *hip_stream);
+
+/* Gradient of ink_rms_norm with y of `type`: dx (of x and of the residual alike) [rows][cols] of `type`, dweight [cols] of `param_type`,
+ * summed over the rows; each may be NULL (not wanted).  total is t (x where there was no residual), rstd as the forward call wrote it;
+ * d_total, the gradient that arrives at t from elsewhere, is added to dx (NULL: none). */
+size_t ink_rms_norm_backward_work(int64_t rows, int32_t cols, int32_t type);
+ink_status ink_rms_norm_backward(const void *dy, int64_t ld_dy, const void *total, int64_t ld_total, const float *rstd, const void *weight,
+                                 const void *d_total, int64_t ld_dt, int64_t rows, int32_t cols, int32_t type, int32_t param_type, void *dx,
+                                 int64_t ld_dx, void *dweight, void *work, size_t work_bytes, void *hip_stream);
+
+/* The gated pair of projections, h = act(x Wg) * (x Wu).
+ *   x            [rows][cols] of `type`;  w_gate (Wg), w_up (Wu) [cols][hidden] of `type`;  cols and hidden 1 .. INK_MAX_IN_DIM
+ *   h            [rows][hidden] of `out_type`, which is `type`
+ *   act          ink_act
+ * Of 8-bit rows (type INK_E4M3, ink_rms_norm's): row r of x is x_scale[r] times its numbers; the weights lie column by column,
+ * [hidden][cols], and column c of Wg is gate_scale[c] times its numbers, of Wu up_scale[c] times; out_type is any of the other three.  The
+ * scales are float and not read for other types. */
+ink_status ink_gated(const void *x, int64_t ld_x, const float *x_scale, const void *w_gate, int64_t ld_gate, const void *w_up,
+                     int64_t ld_up, const float *gate_scale, const float *up_scale, int64_t rows, int32_t cols, int32_t hidden, int32_t type,
+                     int32_t out_type, int32_t act, void *h, int64_t ld_h, void *hip_stream);
+
+/* Gradient of ink_gated (not of 8-bit rows), with g = x Wg and u = x Wu formed anew: dg = dh u act'(g), du = dh act(g), dx = dg Wg^T + du Wu^T
+ * [rows][cols], dw_gate = x^T dg and dw_up = x^T du [cols][hidden], all of `type`; each may be NULL (not wanted).  With 16-bit rows
+ * dg and du are rounded to `type` before the products.  The work memory does not grow with the rows beyond some 200 MB. */
+size_t ink_gated_backward_work(int64_t rows, int32_t cols, int32_t hidden, int32_t type);
+ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int64_t ld_x, const void *w_gate, int64_t ld_gate,
+                              const void *w_up, int64_t ld_up, int64_t rows, int32_t cols, int32_t hidden, int32_t type, int32_t act, void *dx,
+                              int64_t ld_dx, void *dw_gate, int64_t ld_dg, void *dw_up, int64_t ld_du, void *work, size_t work_bytes,
+                              void *hip_stream);
+
+/* One step of AdamW over n_tensors tensors, in place: with g = grad * grad_scale (times *grad_scale_at where that is not NULL) and t the step,
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps).
+ *   tensors      HOST array, read before the call returns; what its entries point to is DEVICE memory.  No tensor may stand there twice
+ *   param_type   INK_F32 or INK_BF16;  grad_type any;  copy_type INK_BF16 or INK_F16 with INK_F32 parameters, or INK_NO_TYPE
+ *   moment_bits  32: m and v are float arrays.  8: m and v are INK_E4M3 arrays, and of each INK_ADAMW_BLOCK neighbouring elements m is
+ *                m_scale times the number of its code, sqrt(v) v_scale times that of its code; zeros everywhere are the moments at the start
+ *   step         t, from 1; or step_at, one int64 on the device that holds it (a captured call reads it at every replay; below 1 counts as 1)
+ *   seed         of the random numbers that round 8-bit moments and INK_BF16 parameters: up or down, in proportion (unbiased).  The
+ *                numbers depend on seed, t, the tensor's id and the element, and on nothing else
+ *   lr and weight_decay >= 0;  betas in [0, 1);  eps > 0
+ * A gradient that is NaN or infinite makes its element NaN, with 8-bit moments the moments of its block. */
+typedef struct {
+  void *param;
+  const void *grad;
+  void *copy;                /* gets the new parameters, rounded to nearest; with copy_type only */
+  void *m, *v;
+  float *m_scale, *v_scale;  /* 8 bits only: [(n + INK_ADAMW_BLOCK - 1) / INK_ADAMW_BLOCK] */
+  int64_t n;                 /* elements; 0: nothing is done */
+  int64_t id;                /* its low 32 bits tell the tensor's random numbers from those of others */
+} ink_adamw_tensor;
+ink_status ink_adamw(const ink_adamw_tensor *tensors, int32_t n_tensors, int32_t param_type, int32_t grad_type, int32_t copy_type,
+                     int32_t moment_bits, double lr, double beta1, double beta2, double eps, double weight_decay, int64_t step,
+                     const int64_t *step_at, double grad_scale, const float *grad_scale_at, uint64_t seed, void *hip_stream);
 
 /* Message of the last failing call on this context ("" if none).  ctx may be NULL: then the
  * message of the last failing ink_create or operator of an answer head on this thread. */

@@ -1,0 +1,676 @@
+// The gated pair of projections, h = act(x Wg) * (x Wu), and its gradient.
+//
+//   forward   g = x Wg, u = x Wu (8-bit rows and weights: times the row's and the column's scale),  h = act(g) u
+//   gradient  g and u formed anew from x;  dg = dh u act'(g), du = dh act(g);
+//             dx = dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du
+#include <algorithm>
+#include <type_traits>
+
+#include "matrix.h"
+
+namespace ink {
+
+// 8-bit operands.  The matrix instructions of 8-bit floats align the products that they add up at once to the largest and drop what lies some 14 bits
+// below it (measured: beside 448 * 448 the product 8 counts, 4 does not), which makes 1.4e-5 of a sum of 64 to 1024 products.  That is a hundredth of
+// the rounding of a bfloat16 result and a tenth of a float16 one; 32-bit results are formed in bfloat16, which holds every e4m3 number and
+// whose products and sums are exact and in 32 bits, at half the rate.
+typedef uint8_t e4m3;                        // held as its bits
+template <> struct Frag<e4m3> { typedef int V __attribute__((ext_vector_type(8))); };      // 32 elements a lane
+__device__ __forceinline__ f32x16 mma(Frag<e4m3>::V a, Frag<e4m3>::V b, f32x16 c) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);       // both e4m3, no block scales
+}
+
+typedef int Piece __attribute__((ext_vector_type(4)));                // 16 bytes
+typedef int PieceAny __attribute__((ext_vector_type(4), aligned(1)));
+
+// Elements k .. of a row of n elements, as many as a piece holds; past the row's end zeros, and nothing is read there.
+template <class T> __device__ __forceinline__ Piece row_piece(const T *row, int k, int n) {
+  constexpr int N = 16 / sizeof(T);
+  if (k + N <= n) return (Piece)*reinterpret_cast<const PieceAny *>(row + k);
+  Piece v{};
+  if constexpr (sizeof(T) == 1) {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < N; j++)
+      if (k + j < n) w[j / 4] |= (uint32_t)row[k + j] << 8 * (j % 4);
+#pragma unroll
+    for (int j = 0; j < 4; j++) v[j] = (int)w[j];
+  } else {
+    typedef T R __attribute__((ext_vector_type(N)));
+    R r{};
+#pragma unroll
+    for (int j = 0; j < N; j++) r[j] = k + j < n ? row[k + j] : (T)0.f;
+    v = __builtin_bit_cast(Piece, r);
+  }
+  return v;
+}
+
+// Elements k .. of a row of TL as a piece of T: 8-bit numbers may become 16-bit ones on the way.
+template <class TL, class T> __device__ __forceinline__ Piece row_piece_as(const TL *row, int k, int n) {
+  if constexpr (sizeof(TL) == sizeof(T)) return row_piece(row, k, n);
+  else {
+    uint32_t w[2] = {0, 0};
+    if (k + 8 <= n) {
+      typedef uint32_t W __attribute__((ext_vector_type(2), aligned(1)));
+      const W v = *reinterpret_cast<const W *>(row + k);
+      w[0] = v[0]; w[1] = v[1];
+    } else
+#pragma unroll
+      for (int j = 0; j < 8; j++)
+        if (k + j < n) w[j / 4] |= (uint32_t)row[k + j] << 8 * (j % 4);
+    typedef T R __attribute__((ext_vector_type(8)));
+    R r;
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
+      r[4 * j] = (T)lo[0]; r[4 * j + 1] = (T)lo[1]; r[4 * j + 2] = (T)hi[0]; r[4 * j + 3] = (T)hi[1];
+    }
+    return __builtin_bit_cast(Piece, r);
+  }
+}
+
+struct GatedArgs {
+  const void *x, *gate, *up, *dh;
+  const float *x_scale, *gate_scale, *up_scale;
+  void *out;                                 // forward: h; gradient: [rows][2 pad] of dg and du
+  int64_t rows, ld_x, ld_gate, ld_up, ld_dh, ld_out;
+  int cols, hidden, act, pad;                // pad: hidden rounded up to whole tiles
+};
+
+constexpr int kChunk = 128, kChunkPitch = kChunk + 16;     // bytes of the depth in LDS at a time, and between rows there
+constexpr int kTileHidden = 64;                            // columns of Wg and of Wu a tile takes
+
+template <class T> constexpr int kTypeStep = sizeof(T) == 1 ? 64 : 32 / (int)sizeof(T);    // depth of a matrix instruction's fragments
+template <class T> constexpr int kChunkK = kChunk / (int)sizeof(T);
+
+// Fragment of step s of 32 rows of an operand whose depth runs along its rows in LDS.
+template <class T> __device__ __forceinline__ typename Frag<T>::V rows_frag(const char *rows, int pitch, int s) {
+  const int l = lane_id(), half = l / 32;
+  const char *at = rows + (l % 32) * pitch;
+  if constexpr (sizeof(T) == 1) {
+    const Piece a = *reinterpret_cast<const Piece *>(at + s * 64 + half * 32), b = *reinterpret_cast<const Piece *>(at + s * 64 + half * 32 + 16);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  } else return *reinterpret_cast<const typename Frag<T>::V *>(at + s * 32 + half * 16);
+}
+// The same of 32 columns of an operand whose depth runs down its columns, with the depth in the order that rows_frag has it.
+template <class T> __device__ __forceinline__ typename Frag<T>::V deep_frag(const char *rows, int pitch, int s, int tile) {
+  if constexpr (sizeof(T) == 2) return columns_frag<T>(rows, pitch, s, tile);
+  else {
+    const int l = lane_id(), half = l / 32;
+    typename Frag<T>::V v;
+#pragma unroll
+    for (int j = 0; j < 4; j++) v[j] = *reinterpret_cast<const float *>(rows + (s * 8 + half * 4 + j) * pitch + (tile * 32 + l % 32) * 4);
+    return v;
+  }
+}
+
+// h of four neighbouring columns
+__device__ __forceinline__ void gate4(float g[4], const float u[4], int act) {
+  activate_all<4>(g, act);
+#pragma unroll
+  for (int j = 0; j < 4; j++) g[j] *= u[j];
+}
+// dg and du in place of g and u
+__device__ __forceinline__ void gate4_grad(float g[4], float u[4], const float dh[4], int act) {
+  float du[4];
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    du[j] = g[j];
+    u[j] *= dh[j];
+  }
+  activate_all<4>(du, act);
+  if (act != INK_ACT_NONE) scale_by_slope<4>(u, g, act);
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    g[j] = u[j];
+    u[j] = du[j] * dh[j];
+  }
+}
+
+// ------------------------------------------------------------------------------------ tiles
+// 64 RB rows by 64 columns of h a workgroup, 32 RB by 32 a wave (a tile of Wg and one of Wu, so that g and u of an element meet in a lane).
+// TL: type of the operands in memory, T: in the products, TO: of h.  GRAD: dg and du go to `out` in place of h.
+template <class TL, class T, class TO, int RB, bool GRAD>
+__global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
+  typedef typename Frag<T>::V V;
+  constexpr int BM = 64 * RB, KC = kChunkK<T>, PE = 16 / sizeof(T), STEPS = KC / kTypeStep<T>;
+  constexpr bool DEEP = sizeof(TL) != 1;     // the depth runs down the weights' columns
+  constexpr int PW = DEEP ? 2 * kTileHidden * (int)sizeof(T) + 16 : kChunkPitch;
+  constexpr int NX = BM * 8 / 256, NW = 4;
+  constexpr int PO = kTileHidden * (int)sizeof(TO) + 16;
+  constexpr int kLoop = BM * kChunkPitch + (DEEP ? KC : 2 * kTileHidden) * PW, kEnd = BM * PO * (GRAD ? 2 : 1);
+  __shared__ __align__(16) char s_mem[kLoop > kEnd ? kLoop : kEnd];
+  char *s_x = s_mem, *s_w = s_mem + BM * kChunkPitch;
+  const int tid = threadIdx.x, l = lane_id(), half = l / 32, wm = tid / kWave / 2, wn = tid / kWave % 2;
+  // workgroups go to the eight chiplets in turn: the column tiles of the same rows are eight apart, so that one L2 serves them
+  const int gy = (a.hidden + kTileHidden - 1) / kTileHidden, id = blockIdx.x / 8;
+  const int64_t m0 = ((int64_t)(id / gy) * 8 + blockIdx.x % 8) * BM;
+  const int n0 = id % gy * kTileHidden;
+  if (m0 >= a.rows) return;
+  Piece x[NX], w[NW];
+  const TL *xp[NX];
+#pragma unroll
+  for (int j = 0; j < NX; j++) xp[j] = static_cast<const TL *>(a.x) + min(m0 + tid / 8 + 32 * j, a.rows - 1) * a.ld_x;
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int j = 0; j < NX; j++) x[j] = row_piece_as<TL, T>(xp[j], k0 + tid % 8 * PE, a.cols);
+#pragma unroll
+    for (int j = 0; j < NW; j++) {
+      const int i = tid + 256 * j;
+      w[j] = Piece{};
+      if constexpr (DEEP) {
+        constexpr int C = kTileHidden / PE;    // pieces of a row of Wg
+        const int k = k0 + i / (2 * C), c = i % (2 * C), n = n0 + c % C * PE;
+        const TL *row = static_cast<const TL *>(c < C ? a.gate : a.up) + (int64_t)k * (c < C ? a.ld_gate : a.ld_up);
+        if (k < a.cols && n < a.hidden) w[j] = row_piece_as<TL, T>(row, n, a.hidden);
+      } else {
+        const int c = i / 8, n = n0 + c % kTileHidden;
+        const TL *row = static_cast<const TL *>(c < kTileHidden ? a.gate : a.up) + (int64_t)n * (c < kTileHidden ? a.ld_gate : a.ld_up);
+        if (n < a.hidden) w[j] = row_piece_as<TL, T>(row, k0 + i % 8 * PE, a.cols);
+      }
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int j = 0; j < NX; j++) *reinterpret_cast<Piece *>(s_x + (tid / 8 + 32 * j) * kChunkPitch + tid % 8 * 16) = x[j];
+#pragma unroll
+    for (int j = 0; j < NW; j++) {
+      const int i = tid + 256 * j;
+      constexpr int C = DEEP ? 2 * kTileHidden / PE : 8;
+      *reinterpret_cast<Piece *>(s_w + i / C * PW + i % C * 16) = w[j];
+    }
+  };
+  f32x16 g[RB], u[RB];
+#pragma unroll
+  for (int i = 0; i < RB; i++) g[i] = u[i] = f32x16{};
+  fetch(0);
+  put();
+  __syncthreads();
+  for (int k0 = 0; k0 < a.cols; k0 += KC) {
+    const bool more = k0 + KC < a.cols;
+    if (more) fetch(k0 + KC);
+#pragma unroll
+    for (int s = 0; s < STEPS; s++) {
+      V ws[2], xs[RB];
+      if constexpr (DEEP) {
+        ws[0] = deep_frag<T>(s_w, PW, s, wn);
+        ws[1] = deep_frag<T>(s_w, PW, s, 2 + wn);
+      } else {
+        ws[0] = rows_frag<T>(s_w + wn * 32 * PW, PW, s);
+        ws[1] = rows_frag<T>(s_w + (kTileHidden + wn * 32) * PW, PW, s);
+      }
+#pragma unroll
+      for (int i = 0; i < RB; i++) xs[i] = rows_frag<T>(s_x + (wm * RB + i) * 32 * kChunkPitch, kChunkPitch, s);
+      if constexpr (sizeof(T) == 4) {          // the four instructions of a step take turns among the accumulators
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+          for (int i = 0; i < RB; i++) {
+            g[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(ws[0][j], xs[i][j], g[i], 0, 0, 0);
+            u[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(ws[1][j], xs[i][j], u[i], 0, 0, 0);
+          }
+      } else
+#pragma unroll
+        for (int i = 0; i < RB; i++) {
+          g[i] = mma(ws[0], xs[i], g[i]);
+          u[i] = mma(ws[1], xs[i], u[i]);
+        }
+    }
+    __syncthreads();
+    if (more) put();
+    __syncthreads();
+  }
+  // Through LDS, so that dh is read and h, dg and du are written in whole lines.
+  constexpr int OE = 16 / sizeof(TO), OP = kTileHidden / OE, NO = BM * OP / 256;      // elements of a piece, pieces of a row, pieces a thread
+  if constexpr (GRAD) {
+#pragma unroll
+    for (int j = 0; j < NO; j++) {
+      const int i = tid + 256 * j, row = i / OP, c = i % OP;
+      const int64_t r = min(m0 + row, a.rows - 1);
+      Piece v{};
+      if (n0 + c * OE < a.hidden) v = row_piece(static_cast<const TO *>(a.dh) + r * a.ld_dh, n0 + c * OE, a.hidden);
+      *reinterpret_cast<Piece *>(s_mem + row * PO + c * 16) = v;
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < RB; i++) {
+    const int row = (wm * RB + i) * 32 + l % 32;
+    float scale = 1.f;
+    if constexpr (!DEEP) scale = a.x_scale[min(m0 + row, a.rows - 1)];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      const int c = wn * 32 + 8 * e + 4 * half;
+      float gv[4], uv[4];
+#pragma unroll
+      for (int j = 0; j < 4; j++) { gv[j] = g[i][4 * e + j]; uv[j] = u[i][4 * e + j]; }
+      if constexpr (!DEEP) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const int n = min(n0 + c + j, a.hidden - 1);
+          gv[j] *= scale * a.gate_scale[n];
+          uv[j] *= scale * a.up_scale[n];
+        }
+      }
+      TO *at = reinterpret_cast<TO *>(s_mem + row * PO) + c;
+      if constexpr (GRAD) {
+        float dh[4];
+        load_pack<TO, 4>(at, dh);
+        gate4_grad(gv, uv, dh, a.act);
+        if (n0 + kTileHidden > a.hidden)       // behind the last column the products that follow find zeros, whatever x holds
+#pragma unroll
+          for (int j = 0; j < 4; j++)
+            if (n0 + c + j >= a.hidden) gv[j] = uv[j] = 0.f;
+        store_pack<TO, 4>(reinterpret_cast<TO *>(s_mem + (BM + row) * PO) + c, uv);
+      } else gate4(gv, uv, a.act);
+      store_pack<TO, 4>(at, gv);
+    }
+  }
+  __syncthreads();
+  if constexpr (GRAD) {
+#pragma unroll
+    for (int j = 0; j < 2 * NO; j++) {
+      const int i = tid + 256 * j, row = i / OP, c = i % OP, part = row / BM;
+      const int64_t r = m0 + row % BM;
+      if (r < a.rows)
+        *reinterpret_cast<Piece *>(static_cast<TO *>(a.out) + r * a.ld_out + part * a.pad + n0 + c * OE) = *reinterpret_cast<const Piece *>(s_mem + row * PO + c * 16);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NO; j++) {
+      const int i = tid + 256 * j, row = i / OP, c = i % OP, n = n0 + c * OE;
+      const int64_t r = m0 + row;
+      if (r >= a.rows || n >= a.hidden) continue;
+      const Piece v = *reinterpret_cast<const Piece *>(s_mem + row * PO + c * 16);
+      TO *to = static_cast<TO *>(a.out) + r * a.ld_out + n;
+      if (n + OE <= a.hidden) *reinterpret_cast<PieceAny *>(to) = v;
+      else {
+        const TO *from = reinterpret_cast<const TO *>(s_mem + row * PO) + c * OE;
+        for (int e = 0; n + e < a.hidden; e++) to[e] = from[e];
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------ gradient
+// dx = dg Wg^T + du Wu^T of the rows of one call of k_gated_tile: 128 rows by 128 columns a workgroup, 64 by 64 a wave.
+struct GatedDxArgs {
+  const void *d, *gate, *up;                 // [rows][2 pad] of dg and du
+  void *dx;
+  int64_t rows, ld_gate, ld_up, ld_dx;
+  int cols, hidden, pad;
+};
+template <class T>
+__global__ __launch_bounds__(256, 2) void k_gated_dx(GatedDxArgs a) {
+  typedef typename Frag<T>::V V;
+  constexpr int KC = kChunkK<T>, PE = 16 / sizeof(T), BM = 128, BN = 128, P = kChunkPitch;
+  constexpr int PO = BN * (int)sizeof(T) + 16, kLoop = (BM + BN) * P, kEnd = BM * PO;
+  __shared__ __align__(16) char s_mem[kLoop > kEnd ? kLoop : kEnd];
+  char *s_d = s_mem, *s_w = s_mem + BM * P;
+  const int tid = threadIdx.x, l = lane_id(), half = l / 32, wm = tid / kWave / 2, wn = tid / kWave % 2;
+  const int gy = (a.cols + BN - 1) / BN, id = blockIdx.x / 8;
+  const int64_t m0 = ((int64_t)(id / gy) * 8 + blockIdx.x % 8) * BM;
+  const int n0 = id % gy * BN;
+  if (m0 >= a.rows) return;
+  Piece d[4], w[4];
+  const T *dp[4];
+#pragma unroll
+  for (int j = 0; j < 4; j++) dp[j] = static_cast<const T *>(a.d) + min(m0 + tid / 8 + 32 * j, a.rows - 1) * 2 * a.pad;
+  auto fetch = [&](int k0) {
+    const bool second = k0 >= a.pad;
+    const int k = k0 - (second ? a.pad : 0) + tid % 8 * PE;
+    const T *from = static_cast<const T *>(second ? a.up : a.gate);
+    const int64_t ld = second ? a.ld_up : a.ld_gate;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      d[j] = *reinterpret_cast<const Piece *>(dp[j] + k0 + tid % 8 * PE);
+      const int n = n0 + tid / 8 + 32 * j;
+      w[j] = Piece{};
+      if (n < a.cols && k < a.hidden) w[j] = row_piece(from + (int64_t)n * ld, k, a.hidden);
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      *reinterpret_cast<Piece *>(s_d + (tid / 8 + 32 * j) * P + tid % 8 * 16) = d[j];
+      *reinterpret_cast<Piece *>(s_w + (tid / 8 + 32 * j) * P + tid % 8 * 16) = w[j];
+    }
+  };
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; i++) acc[i][0] = acc[i][1] = f32x16{};
+  fetch(0);
+  put();
+  __syncthreads();
+  for (int k0 = 0; k0 < 2 * a.pad; k0 += KC) {
+    const bool more = k0 + KC < 2 * a.pad;
+    if (more) fetch(k0 + KC);
+#pragma unroll
+    for (int s = 0; s < 4; s++) {
+      V ds[2], ws[2];
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        ds[i] = rows_frag<T>(s_d + (wm * 2 + i) * 32 * P, P, s);
+        ws[i] = rows_frag<T>(s_w + (wn * 2 + i) * 32 * P, P, s);
+      }
+      mma_block<T>(ws, ds, acc);
+    }
+    __syncthreads();
+    if (more) put();
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+#pragma unroll
+    for (int n = 0; n < 2; n++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const float v[4] = {acc[i][n][4 * e], acc[i][n][4 * e + 1], acc[i][n][4 * e + 2], acc[i][n][4 * e + 3]};
+        store_pack<T, 4>(reinterpret_cast<T *>(s_mem + ((wm * 2 + i) * 32 + l % 32) * PO) + (wn * 2 + n) * 32 + 8 * e + 4 * half, v);
+      }
+  __syncthreads();
+  constexpr int OP = BN / PE;
+#pragma unroll
+  for (int j = 0; j < BM * OP / 256; j++) {
+    const int i = tid + 256 * j, row = i / OP, c = i % OP, n = n0 + c * PE;
+    const int64_t r = m0 + row;
+    if (r >= a.rows || n >= a.cols) continue;
+    T *to = static_cast<T *>(a.dx) + r * a.ld_dx + n;
+    if (n + PE <= a.cols) *reinterpret_cast<PieceAny *>(to) = *reinterpret_cast<const Piece *>(s_mem + row * PO + c * 16);
+    else {
+      const T *from = reinterpret_cast<const T *>(s_mem + row * PO) + c * PE;
+      for (int e = 0; n + e < a.cols; e++) to[e] = from[e];
+    }
+  }
+}
+
+// Sums over the rows of one call of k_gated_tile, x^T [dg du]: 128 columns of x by 128 of dg and du a workgroup, over a slice of the rows.  The sums of
+// the slice go to, or are added to, its partial matrix, in the fragments' order.
+struct GatedDwArgs {
+  const void *x, *d;
+  float *part;                               // [slices][tiles of x][tiles of d][4 fragments a wave, 4 waves]
+  int64_t rows, ld_x, slice;
+  int cols, pad, add;
+};
+template <class T>
+__global__ __launch_bounds__(256, 2) void k_gated_dw(GatedDwArgs a) {
+  typedef typename Frag<T>::V V;
+  constexpr int KR = kChunkK<T>, PE = 16 / sizeof(T), P = kGradPitch<T, 4>, C = 128 / PE, STEPS = KR / kStep<T>;      // rows at a time, pieces of a row
+  __shared__ __align__(16) char s_x[KR * P], s_d[KR * P];
+  const int tid = threadIdx.x, l = lane_id(), wm = tid / kWave / 2, wn = tid / kWave % 2;
+  const int c0 = blockIdx.x * 128, n0 = blockIdx.y * 128;
+  const int64_t r_begin = blockIdx.z * a.slice, r_end = min(r_begin + a.slice, a.rows);
+  float *part = a.part + (((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * gridDim.y + blockIdx.y) * 16384;
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+#pragma unroll
+    for (int n = 0; n < 2; n++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        F4 v = F4{};
+        if (a.add) v = reinterpret_cast<const F4 *>(part)[(((wm * 2 + i) * 4 + wn * 2 + n) * 4 + e) * 64 + l];
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][n][4 * e + j] = v[j];
+      }
+  Piece x[4], d[4];
+  auto fetch = [&](int64_t r0) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const int i = tid + 256 * j, c = i % C * PE;
+      const int64_t r = r0 + i / C;
+      x[j] = d[j] = Piece{};
+      if (r >= r_end) continue;
+      if (c0 + c < a.cols) x[j] = row_piece(static_cast<const T *>(a.x) + r * a.ld_x, c0 + c, a.cols);
+      if (n0 + c < 2 * a.pad) d[j] = *reinterpret_cast<const Piece *>(static_cast<const T *>(a.d) + r * 2 * a.pad + n0 + c);
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const int i = tid + 256 * j;
+      *reinterpret_cast<Piece *>(s_x + i / C * P + i % C * 16) = x[j];
+      *reinterpret_cast<Piece *>(s_d + i / C * P + i % C * 16) = d[j];
+    }
+  };
+  fetch(r_begin);
+  put();
+  __syncthreads();
+  for (int64_t r0 = r_begin; r0 < r_end; r0 += KR) {
+    const bool more = r0 + KR < r_end;
+    if (more) fetch(r0 + KR);
+#pragma unroll
+    for (int s = 0; s < STEPS; s++) {
+      V xs[2], ds[2];
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        xs[i] = columns_frag<T>(s_x, P, s, wm * 2 + i);
+        ds[i] = columns_frag<T>(s_d, P, s, wn * 2 + i);
+      }
+      mma_block<T>(ds, xs, acc);
+    }
+    __syncthreads();
+    if (more) put();
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+#pragma unroll
+    for (int n = 0; n < 2; n++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const F4 v = {acc[i][n][4 * e], acc[i][n][4 * e + 1], acc[i][n][4 * e + 2], acc[i][n][4 * e + 3]};
+        reinterpret_cast<F4 *>(part)[(((wm * 2 + i) * 4 + wn * 2 + n) * 4 + e) * 64 + l] = v;
+      }
+}
+
+// Partial matrices to the weights' gradients: 64 elements, four by four, a workgroup; 16 threads share a sum, in the slices' order.
+struct GatedSumArgs {
+  const float *part;
+  void *d_gate, *d_up;
+  int64_t ld_gate, ld_up;
+  int slices, type, cols, hidden, pad, tiles_c, tiles_n;
+};
+__global__ __launch_bounds__(256) void k_gated_sum(GatedSumArgs a) {
+  __shared__ F4 s[16][17];
+  const int x = threadIdx.x % 16, y = threadIdx.x / 16;
+  const int64_t n = (int64_t)a.tiles_c * a.tiles_n * 16384, i = ((int64_t)blockIdx.x * 16 + x) * 4;
+  F4 t = F4{};
+#pragma unroll 4
+  for (int p = y; p < a.slices; p += 16) t += *reinterpret_cast<const F4 *>(a.part + p * n + i);
+  s[y][x] = t;
+  __syncthreads();
+  if (y) return;
+  t = F4{};
+#pragma unroll
+  for (int p = 0; p < 16; p++) t += s[p][x];
+  const int tile = (int)(i / 16384), f = (int)(i % 16384), frag = f / 1024, e = f / 256 % 4, lane = f / 4 % 64;
+  const int c = tile / a.tiles_n * 128 + frag / 4 * 32 + lane % 32;
+  int h = tile % a.tiles_n * 128 + frag % 4 * 32 + 8 * e + 4 * (lane / 32);
+  const bool up = h >= a.pad;
+  if (up) h -= a.pad;
+  void *out = up ? a.d_up : a.d_gate;
+  if (c >= a.cols || !out) return;
+  for (int j = 0; j < 4; j++)
+    if (h + j < a.hidden) store_any(out, (int64_t)c * (up ? a.ld_up : a.ld_gate) + h + j, a.type, t[j]);
+}
+
+// ------------------------------------------------------------------------------------ a few rows
+// One row and 32 columns of h a workgroup: lanes side by side take 16 bytes of a row of Wg and of Wu, the rest of the workgroup splits the depth.
+template <class T>
+__global__ __launch_bounds__(kHeadThreads) void k_gated_few(GatedArgs a) {
+  constexpr int VK = kVec<T>, CL = 32 / VK, SL = kHeadThreads / CL, W = kHeadThreads / kWave;
+  __shared__ float s_sum[2][W][32];
+  const int cl = threadIdx.x % CL, sl = threadIdx.x / CL, n0 = blockIdx.x * 32, n = n0 + cl * VK;
+  const int64_t r = blockIdx.y;
+  const T *x = static_cast<const T *>(a.x) + r * a.ld_x, *wg = static_cast<const T *>(a.gate), *wu = static_cast<const T *>(a.up);
+  float g[VK], u[VK];
+#pragma unroll
+  for (int j = 0; j < VK; j++) g[j] = u[j] = 0.f;
+  if (n < a.hidden)
+#pragma unroll 4
+    for (int k = sl; k < a.cols; k += SL) {
+      const float xv = (float)x[k];
+      const typename Frag<T>::V vg = row_frag<T>(wg + (int64_t)k * a.ld_gate, n, a.hidden), vu = row_frag<T>(wu + (int64_t)k * a.ld_up, n, a.hidden);
+#pragma unroll
+      for (int j = 0; j < VK; j++) {
+        g[j] = fmaf(xv, (float)vg[j], g[j]);
+        u[j] = fmaf(xv, (float)vu[j], u[j]);
+      }
+    }
+#pragma unroll
+  for (int j = 0; j < VK; j++) {
+#pragma unroll
+    for (int o = CL; o < kWave; o <<= 1) { g[j] += __shfl_xor(g[j], o, kWave); u[j] += __shfl_xor(u[j], o, kWave); }
+    if (lane_id() < CL) { s_sum[0][threadIdx.x / kWave][cl * VK + j] = g[j]; s_sum[1][threadIdx.x / kWave][cl * VK + j] = u[j]; }
+  }
+  __syncthreads();
+  const int c = n0 + threadIdx.x;
+  if (threadIdx.x >= 32 || c >= a.hidden) return;
+  float gv = 0.f, uv = 0.f;
+#pragma unroll
+  for (int i = 0; i < W; i++) { gv += s_sum[0][i][threadIdx.x]; uv += s_sum[1][i][threadIdx.x]; }
+  static_cast<T *>(a.out)[r * a.ld_out + c] = (T)(activate(gv, a.act) * uv);
+}
+
+// ------------------------------------------------------------------------------------ host side
+constexpr int64_t kFewRows = 16, kFewResults = 64 * 1024;    // as ink_linear: each workgroup asks for its columns of both matrices again for every row
+
+constexpr int64_t kLaunchRows = 1 << 21;     // a launch has fewer than 2^32 threads: so many rows by INK_MAX_IN_DIM columns are 2^30
+template <class TL, class T, class TO> static void gated_tiles(const GatedArgs &a, Launches &run) {
+  const int gy = (a.hidden + kTileHidden - 1) / kTileHidden;
+  for (int64_t r0 = 0; r0 < a.rows; r0 += kLaunchRows) {
+    GatedArgs b = a;
+    b.rows = std::min(kLaunchRows, a.rows - r0);
+    b.x = static_cast<const TL *>(a.x) + r0 * a.ld_x;
+    b.out = static_cast<TO *>(a.out) + r0 * a.ld_out;
+    if (a.x_scale) b.x_scale = a.x_scale + r0;
+    const int64_t tiles = (b.rows + 127) / 128;
+    run(k_gated_tile<TL, T, TO, 2, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * gy)), dim3(256), b);
+  }
+}
+template <class T, class TO> static void gated_run(const GatedArgs &a, Launches &run) {
+  if constexpr (sizeof(T) != 1)
+    if (a.rows <= kFewRows && a.rows * a.hidden <= kFewResults)
+      return run(k_gated_few<T>, dim3((a.hidden + 31) / 32, (unsigned)a.rows), dim3(kHeadThreads), a);
+  gated_tiles<T, std::conditional_t<sizeof(T) == 1 && sizeof(TO) == 4, bf16, T>, TO>(a, run);
+}
+
+// The gradient takes the rows in parts whose dg and du (2 pad columns) have about 128 MB, so that the products that read them find them in the cache behind
+// the L2s, and the work memory does not grow with the rows.
+struct GatedPlan { int pad, tiles_c, tiles_n, slices; int64_t part_rows, slice, d_bytes, part_bytes; };
+static GatedPlan gated_plan(int64_t rows, int cols, int hidden, int type) {
+  GatedPlan p{};
+  p.pad = (hidden + kTileHidden - 1) / kTileHidden * kTileHidden;
+  const int64_t row_bytes = 2ll * p.pad * type_size(type);
+  p.part_rows = std::min((rows + 127) / 128 * 128, std::max<int64_t>(1024, (128 << 20) / row_bytes / 1024 * 1024));
+  p.tiles_c = (cols + 127) / 128;
+  p.tiles_n = (2 * p.pad + 127) / 128;
+  const int64_t steps = p.part_rows / 64, tiles = (int64_t)p.tiles_c * p.tiles_n;     // 64 rows: whole chunks of every type
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(steps / 2, 1024 / tiles));
+  p.slice = (steps + slices - 1) / slices * 64;
+  p.slices = (int)((p.part_rows + p.slice - 1) / p.slice);
+  p.d_bytes = p.part_rows * row_bytes;
+  p.part_bytes = (int64_t)p.slices * tiles * 16384 * 4;
+  return p;
+}
+
+template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void *work, void *dx, int64_t ld_dx, bool weights, Launches &run) {
+  const int64_t rows = a.rows;
+  a.out = work; a.ld_out = 2 * p.pad; a.pad = p.pad;
+  for (int64_t r0 = 0; r0 < rows; r0 += p.part_rows) {
+    GatedArgs b = a;
+    b.rows = std::min(p.part_rows, rows - r0);
+    b.x = static_cast<const T *>(a.x) + r0 * a.ld_x;
+    b.dh = static_cast<const T *>(a.dh) + r0 * a.ld_dh;
+    const int64_t tiles = (b.rows + 127) / 128;
+    run(k_gated_tile<T, T, T, 2, true>, dim3((unsigned)((tiles + 7) / 8 * 8 * (p.pad / kTileHidden))), dim3(256), b);
+    if (dx) {
+      GatedDxArgs q{work, a.gate, a.up, static_cast<T *>(dx) + r0 * ld_dx, b.rows, a.ld_gate, a.ld_up, ld_dx, a.cols, a.hidden, p.pad};
+      run(k_gated_dx<T>, dim3((unsigned)((tiles + 7) / 8 * 8 * p.tiles_c)), dim3(256), q);
+    }
+    if (weights) {
+      GatedDwArgs q{b.x, work, reinterpret_cast<float *>(static_cast<char *>(work) + p.d_bytes), b.rows, a.ld_x, p.slice, a.cols, p.pad, r0 > 0};
+      run(k_gated_dw<T>, dim3(p.tiles_c, p.tiles_n, p.slices), dim3(256), q);
+    }
+  }
+}
+
+static const char *gated_check(int64_t rows, int32_t cols, int32_t hidden, int32_t act) {
+  if (act < INK_ACT_NONE || act > INK_ACT_SILU) return "unknown activation";
+  if (rows < 0 || rows > kMaxHeadRows) return "rows out of range";
+  if (cols < 1 || cols > INK_MAX_IN_DIM || hidden < 1 || hidden > INK_MAX_IN_DIM) return "cols and hidden must be 1 .. INK_MAX_IN_DIM";
+  return nullptr;
+}
+
+}  // namespace ink
+
+using namespace ink;
+
+extern "C" ink_status ink_gated(const void *x, int64_t ld_x, const float *x_scale, const void *w_gate, int64_t ld_gate, const void *w_up,
+                                int64_t ld_up, const float *gate_scale, const float *up_scale, int64_t rows, int32_t cols, int32_t hidden,
+                                int32_t type, int32_t out_type, int32_t act, void *h, int64_t ld_h, void *hip_stream) {
+  const char *who = "ink_gated";
+  const bool eight = type == INK_E4M3;
+  if (!known_type(type) && !eight) return fail_call(INK_E_ARG, "%s: unknown type", who);
+  if (eight ? !known_type(out_type) : out_type != type) return fail_call(INK_E_ARG, "%s: the results' type must be the rows' type, of INK_E4M3 rows one of the others", who);
+  if (const char *why = gated_check(rows, cols, hidden, act)) return fail_call(INK_E_ARG, "%s: %s", who, why);
+  const int w_rows = eight ? hidden : cols, w_cols = eight ? cols : hidden;
+  if (!good_matrix(x, rows, cols, ld_x, type, false)) return fail_call(INK_E_ARG, "%s: x is NULL, not aligned to its type or has rows that overlap", who);
+  if (!good_matrix(w_gate, w_rows, w_cols, ld_gate, type, false)) return fail_call(INK_E_ARG, "%s: w_gate is NULL, not aligned to its type or has rows that overlap", who);
+  if (!good_matrix(w_up, w_rows, w_cols, ld_up, type, false)) return fail_call(INK_E_ARG, "%s: w_up is NULL, not aligned to its type or has rows that overlap", who);
+  if (!good_matrix(h, rows, hidden, ld_h, out_type, true)) return fail_call(INK_E_ARG, "%s: h is NULL, not aligned to its type or has rows that overlap", who);
+  if (eight && ((rows > 0 && !x_scale) || !gate_scale || !up_scale || !aligned_to(x_scale, 4) || !aligned_to(gate_scale, 4) || !aligned_to(up_scale, 4)))
+    return fail_call(INK_E_ARG, "%s: a scale is NULL or not aligned", who);
+  if (rows == 0) return INK_OK;
+  GatedArgs a{};
+  a.x = x; a.gate = w_gate; a.up = w_up; a.x_scale = x_scale; a.gate_scale = gate_scale; a.up_scale = up_scale; a.out = h;
+  a.rows = rows; a.ld_x = ld_x; a.ld_gate = ld_gate; a.ld_up = ld_up; a.ld_out = ld_h; a.cols = cols; a.hidden = hidden; a.act = act;
+  Launches run(hip_stream);
+  if (eight) out_type == INK_F32 ? gated_run<e4m3, float>(a, run) : out_type == INK_BF16 ? gated_run<e4m3, bf16>(a, run) : gated_run<e4m3, f16>(a, run);
+  else if (type == INK_F32) gated_run<float, float>(a, run);
+  else type == INK_BF16 ? gated_run<bf16, bf16>(a, run) : gated_run<f16, f16>(a, run);
+  return run.done(who);
+}
+
+extern "C" size_t ink_gated_backward_work(int64_t rows, int32_t cols, int32_t hidden, int32_t type) {
+  if (!known_type(type) || rows < 1 || gated_check(rows, cols, hidden, INK_ACT_NONE)) return 0;
+  const GatedPlan p = gated_plan(rows, cols, hidden, type);
+  return (size_t)(p.d_bytes + p.part_bytes);
+}
+
+extern "C" ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int64_t ld_x, const void *w_gate, int64_t ld_gate,
+                                         const void *w_up, int64_t ld_up, int64_t rows, int32_t cols, int32_t hidden, int32_t type, int32_t act,
+                                         void *dx, int64_t ld_dx, void *dw_gate, int64_t ld_dg, void *dw_up, int64_t ld_du, void *work,
+                                         size_t work_bytes, void *hip_stream) {
+  const char *who = "ink_gated_backward";
+  if (!known_type(type)) return fail_call(INK_E_ARG, "%s: unknown type", who);
+  if (const char *why = gated_check(rows, cols, hidden, act)) return fail_call(INK_E_ARG, "%s: %s", who, why);
+  if (!good_matrix(dh, rows, hidden, ld_dh, type, false)) return fail_call(INK_E_ARG, "%s: dh is NULL, not aligned to its type or has rows that overlap", who);
+  if (!good_matrix(x, rows, cols, ld_x, type, false)) return fail_call(INK_E_ARG, "%s: x is NULL, not aligned to its type or has rows that overlap", who);
+  if (!good_matrix(w_gate, cols, hidden, ld_gate, type, false)) return fail_call(INK_E_ARG, "%s: w_gate is NULL, not aligned to its type or has rows that overlap", who);
+  if (!good_matrix(w_up, cols, hidden, ld_up, type, false)) return fail_call(INK_E_ARG, "%s: w_up is NULL, not aligned to its type or has rows that overlap", who);
+  if (dx && !good_matrix(dx, rows, cols, ld_dx, type, true)) return fail_call(INK_E_ARG, "%s: dx is not aligned to its type or has rows that overlap", who);
+  if (dw_gate && !good_matrix(dw_gate, cols, hidden, ld_dg, type, true)) return fail_call(INK_E_ARG, "%s: dw_gate is not aligned to its type or has rows that overlap", who);
+  if (dw_up && !good_matrix(dw_up, cols, hidden, ld_du, type, true)) return fail_call(INK_E_ARG, "%s: dw_up is not aligned to its type or has rows that overlap", who);
+  const bool weights = dw_gate || dw_up;
+  if (rows > 0 && (dx || weights) && (!work || !aligned_to(work, 16) || work_bytes < ink_gated_backward_work(rows, cols, hidden, type)))
+    return fail_call(INK_E_ARG, "%s: work holds less than ink_gated_backward_work bytes or is not aligned to 16", who);
+  Launches run(hip_stream);
+  GatedPlan p = gated_plan(std::max<int64_t>(rows, 1), cols, hidden, type);
+  if (rows > 0 && (dx || weights)) {
+    GatedArgs a{};
+    a.x = x; a.gate = w_gate; a.up = w_up; a.dh = dh;
+    a.rows = rows; a.ld_x = ld_x; a.ld_gate = ld_gate; a.ld_up = ld_up; a.ld_dh = ld_dh; a.cols = cols; a.hidden = hidden; a.act = act;
+    if (type == INK_F32) gated_grad<float>(a, p, work, dx, ld_dx, weights, run);
+    else type == INK_BF16 ? gated_grad<bf16>(a, p, work, dx, ld_dx, weights, run) : gated_grad<f16>(a, p, work, dx, ld_dx, weights, run);
+  }
+  if (weights) {                             // no rows: zeros
+    GatedSumArgs s{};
+    s.part = reinterpret_cast<const float *>(static_cast<const char *>(work) + p.d_bytes);
+    s.d_gate = dw_gate; s.d_up = dw_up; s.ld_gate = ld_dg; s.ld_up = ld_du; s.slices = rows > 0 ? p.slices : 0; s.type = type;
+    s.cols = cols; s.hidden = hidden; s.pad = p.pad; s.tiles_c = p.tiles_c; s.tiles_n = p.tiles_n;
+    run(k_gated_sum, dim3((unsigned)((int64_t)p.tiles_c * p.tiles_n * 256)), dim3(256), s);
+  }
+  return run.done(who);
+}

@@ -85,7 +85,7 @@ template <int L> __device__ __forceinline__ float block_sum(float x, float *s) {
 // Sets the message that ink_last_error(NULL) returns on this thread.
 ink_status fail_call(ink_status st, const char *fmt, ...) noexcept __attribute__((format(printf, 2, 3)));
 
-inline int type_size(int type) { return type == INK_F32 ? 4 : 2; }
+inline int type_size(int type) { return type == INK_F32 ? 4 : type == INK_E4M3 ? 1 : 2; }
 inline bool known_type(int type) { return type == INK_F32 || type == INK_BF16 || type == INK_F16; }
 inline bool aligned_to(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 

@@ -21,7 +21,7 @@
 // 0.9 and 0.9; bf16 100k x 2100 3.0 and 2.7, 50k x 4096 1.6 and 1.5, 20k x 16384 1.0 and 1.0.
 #include <algorithm>
 
-#include "head.h"
+#include "rowgroup.h"
 
 namespace ink {
 
@@ -34,25 +34,6 @@ struct NormArgs {
   int cols, param_type;
   float eps;
 };
-
-constexpr int kWideThreads = 1024;         // rows that a wave does not hold: one workgroup a row
-
-template <int L> constexpr int norm_threads() { return L > kWave ? L : kHeadThreads; }
-
-// This lane's place in a row: vector i starts at element `at`, its first `skip` elements belong to the vector before.
-template <int L, int V, bool FULL> struct NormPlace {
-  int q, cols;
-  __device__ __forceinline__ NormPlace(int cols_) : q(threadIdx.x % L), cols(cols_) {}
-  __device__ __forceinline__ int first(int i) const { return (i * L + q) * V; }
-  __device__ __forceinline__ int at(int i) const { return FULL ? first(i) : min(first(i), cols - V); }
-  __device__ __forceinline__ bool live(int i, int j) const { return FULL || at(i) + j >= first(i); }
-  __device__ __forceinline__ bool any(int i) const { return FULL || first(i) < cols; }
-};
-
-template <int L> __device__ __forceinline__ float row_sum(float x, float *s) {
-  if constexpr (L > kWave) return block_sum<L>(x, s);
-  else return group_sum<L>(x);
-}
 
 template <class T, int L, int NV, int V, bool FULL>
 __global__ __launch_bounds__(norm_threads<L>()) void k_layer_norm(NormArgs a) {
@@ -191,21 +172,8 @@ __global__ __launch_bounds__(norm_threads<L>()) void k_layer_norm_grad(NormArgs 
 
 // Partial rows to the gradients of weight and bias: 32 columns a workgroup, 32 threads a column.
 __global__ __launch_bounds__(1024) void k_norm_params(const float *part, int n_part, int cols, int param_type, void *dweight, void *dbias) {
-  __shared__ float s[32][33];
   void *out = blockIdx.y ? dbias : dweight;
-  if (!out) return;
-  const int x = threadIdx.x % 32, y = threadIdx.x / 32, c = blockIdx.x * 32 + x;
-  float t = 0.f;
-  if (c < cols)
-#pragma unroll 8
-    for (int i = y; i < n_part; i += 32) t += part[(int64_t)i * 2 * cols + blockIdx.y * cols + c];
-  s[y][x] = t;
-  __syncthreads();
-  if (y) return;
-  t = 0.f;
-#pragma unroll
-  for (int i = 0; i < 32; i++) t += s[i][x];
-  if (c < cols) store_any(out, c, param_type, t);
+  if (out) sum_partial_rows(part + blockIdx.y * cols, n_part, 2 * (int64_t)cols, cols, param_type, out);
 }
 
 // Lanes and loads of a row of n_vec vectors: the smallest group that holds it with at most 4 vectors a lane.

@@ -1,5 +1,5 @@
-"""Operators of an answer head on GPU tensors: layer norm, linear with its epilogue, log probabilities,
-each with its gradient (include/ink.h has what they compute).
+"""Operators of an answer head on GPU tensors: layer norm, root-mean-square norm, linear with its epilogue, gated pairs of
+projections, log probabilities, each with its gradient, and the step of AdamW that uses these (include/ink.h has what they compute).
 
 Argument marshalling only: every operator runs inside libink.so.  Calls are asynchronous on torch's
 current stream of the tensors' device, like torch's own; results and work memory come from torch's
@@ -8,6 +8,7 @@ gradient raises unless it is detached or the call stands under torch.no_grad(). 
 tensor whose rows are contiguous, at any distance from each other; any other layout is copied first.
 Tensors of other devices or types and shapes that do not fit raise.
 """
+import array
 import ctypes as C
 
 import torch
@@ -17,6 +18,8 @@ from .binding import InkError, load_library
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 MAX_TOP = 16
+E4M3 = torch.float8_e4m3fn
+ADAMW_BLOCK = 128       # neighbouring elements whose 8-bit moments share a scale
 
 _fn = None
 
@@ -25,18 +28,24 @@ def _functions():
     global _fn
     if _fn is None:
         lib = load_library()
-        p, i, l, f, z = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
+        p, i, l, f, z, d, n = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t, C.c_double, C.c_uint64
         for name, args in dict(
                 ink_layer_norm=(p, l, p, p, l, i, i, i, f, p, l, p, p, p),
                 ink_layer_norm_backward=(p, l, p, l, p, p, p, l, i, i, i, p, l, p, p, p, z, p),
                 ink_linear=(p, l, p, l, p, p, l, l, i, i, i, i, i, p, l, p, l, p),
                 ink_linear_backward=(p, l, p, l, p, l, p, l, l, i, i, i, i, i, p, l, p, l, p, p, z, p),
                 ink_log_probs=(p, l, p, i, l, l, i, f, i, p, p, p, p, p, p, z, p),
-                ink_log_probs_backward=(p, l, p, i, p, p, p, p, l, l, i, f, p, l, p)).items():
+                ink_log_probs_backward=(p, l, p, i, p, p, p, p, l, l, i, f, p, l, p),
+                ink_rms_norm=(p, l, p, l, p, l, i, i, i, f, i, p, l, p, p, l, p, p),
+                ink_rms_norm_backward=(p, l, p, l, p, p, p, l, l, i, i, i, p, l, p, p, z, p),
+                ink_gated=(p, l, p, p, l, p, l, p, p, l, i, i, i, i, i, p, l, p),
+                ink_gated_backward=(p, l, p, l, p, l, p, l, l, i, i, i, i, p, l, p, l, p, l, p, z, p),
+                ink_adamw=(p, i, i, i, i, i, d, d, d, d, d, l, p, d, p, n, p)).items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, C.c_int
         for name, args in dict(ink_layer_norm_backward_work=(l, i, i), ink_linear_backward_work=(l, i, i),
-                               ink_log_probs_work=(l, l, i, i)).items():
+                               ink_log_probs_work=(l, l, i, i), ink_rms_norm_backward_work=(l, i, i),
+                               ink_gated_backward_work=(l, i, i, i)).items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, z
         _fn = lib
@@ -250,3 +259,246 @@ def log_probs_backward(logits, targets, lse, entropy=None, g_logp=None, g_entrop
     _call(lib.ink_log_probs_backward, logits, logits.data_ptr(), ld, _ptr(targets), 0 if targets is None else targets.element_size(),
           lse.data_ptr(), _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), rows, classes, TYPES[logits.dtype], scale, out.data_ptr(), classes)
     return out
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6, out_dtype=None):
+    """(y, total, rstd) of rows x: total = x + residual in x's type (x itself without a residual), y = total * rstd * weight with
+    rstd = 1 / sqrt(mean of total^2 + eps).  With out_dtype torch.float8_e4m3fn (y, scale, total, rstd): row r of the result is
+    scale[r] times the numbers of y[r].  weight: [cols] of x's type or float32, or None; total and rstd are what the gradient takes."""
+    x, ld = _matrix(x, "x")
+    rows, cols = x.shape
+    t = x.dtype
+    weight = _vector(weight, "weight", cols, x, (t, torch.float32))
+    out_dtype = out_dtype or t
+    if out_dtype is not t and out_dtype is not E4M3:
+        raise TypeError("out_dtype must be x's type or torch.float8_e4m3fn")
+    total, ld_res, scale = x, 0, None
+    if residual is not None:
+        residual, ld_res = _matrix(residual, "residual", rows, cols, t, x)
+        total = x.new_empty((rows, cols))
+    lib = _functions()
+    y = x.new_empty((rows, cols), dtype=out_dtype)
+    rstd = x.new_empty(rows, dtype=torch.float32)
+    if out_dtype is E4M3:
+        scale = x.new_empty(rows, dtype=torch.float32)
+    _call(lib.ink_rms_norm, x, x.data_ptr(), ld, _ptr(residual), ld_res, _ptr(weight), rows, cols, TYPES[t], TYPES[t if weight is None else weight.dtype],
+          eps, _TYPES_8[out_dtype], y.data_ptr(), cols, _ptr(scale), None if residual is None else total.data_ptr(), cols, rstd.data_ptr())
+    return (y, total, rstd) if scale is None else (y, scale, total, rstd)
+
+
+def rms_norm_backward(dy, total, rstd, weight=None, d_total=None, param_dtype=None, need_dx=True, need_dweight=True):
+    """(dx, dweight) of rms_norm; None for what is not needed.  dx is the gradient of x and of the residual alike, d_total (what arrives
+    at the sum from elsewhere, or None) included.  dweight has the weight's type, or param_dtype (total's type or float32)
+    where there is no weight."""
+    total, ld = _matrix(total, "total")
+    rows, cols = total.shape
+    t = total.dtype
+    dy, ld_dy = _matrix(dy, "dy", rows, cols, t, total)
+    rstd = _vector(_given(rstd, "rstd"), "rstd", rows, total, _F32)
+    weight = _vector(weight, "weight", cols, total, (t, torch.float32))
+    ld_dt = 0
+    if d_total is not None:
+        d_total, ld_dt = _matrix(d_total, "d_total", rows, cols, t, total)
+    if weight is not None:
+        if param_dtype not in (None, weight.dtype):
+            raise TypeError("param_dtype differs from the weight's type")
+        param_dtype = weight.dtype
+    elif param_dtype not in (None, t, torch.float32):
+        raise TypeError("param_dtype must be total's type or float32")
+    param_dtype = param_dtype or t
+    lib = _functions()
+    dx = total.new_empty((rows, cols)) if need_dx else None
+    dweight = work = None
+    n_work = 0
+    if need_dweight:
+        dweight = total.new_empty(cols, dtype=param_dtype)
+        n_work = lib.ink_rms_norm_backward_work(rows, cols, TYPES[t])
+        work = total.new_empty(n_work, dtype=torch.uint8) if n_work else None
+    _call(lib.ink_rms_norm_backward, total, dy.data_ptr(), ld_dy, total.data_ptr(), ld, rstd.data_ptr(), _ptr(weight), _ptr(d_total), ld_dt, rows, cols,
+          TYPES[t], TYPES[param_dtype], _ptr(dx), cols, _ptr(dweight), _ptr(work), n_work)
+    return dx, dweight
+
+
+_TYPES_8 = dict(TYPES)
+_TYPES_8[E4M3] = 3
+
+
+def _columns_8(w, name, cols, hidden, like):
+    """8-bit weights [cols, hidden] as memory that holds a column's elements side by side, and the distance of its columns."""
+    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[0] != cols or (hidden is not None and w.shape[1] != hidden) or w.device != like.device:
+        raise ValueError("%s must be a GPU tensor of shape [%d, %s] on the rows' device" % (name, cols, "hidden" if hidden is None else hidden))
+    if w.dtype is not E4M3:
+        raise TypeError("%s has type %s, wanted %s" % (name, w.dtype, E4M3))
+    s0, s1 = w.stride()
+    if (s0 != 1 and cols > 1) or (s1 < cols and s1 != 0 and w.shape[1] > 1):
+        w = w.t().contiguous().t()
+        s1 = cols
+    return w, s1
+
+
+def gated(x, w_gate, w_up, act="silu", x_scale=None, gate_scale=None, up_scale=None, out_dtype=None):
+    """act(x @ w_gate) * (x @ w_up), with weights [cols, hidden] and act none, relu, gelu or silu, in x's type.
+
+    Of 8-bit rows (torch.float8_e4m3fn, rms_norm's) with x_scale [rows] and 8-bit weights with gate_scale and up_scale [hidden] (all
+    float32): rows and weights' columns are their numbers times their scales, and out_dtype is float32, bfloat16 (the default) or
+    float16.  8-bit weights are taken as they are where a column's elements are side by side, as in the transpose of a
+    contiguous [hidden, cols] tensor; any other layout is copied first."""
+    if act not in ACTS:
+        raise ValueError("act must be one of %s" % ", ".join(ACTS))
+    scales = (x_scale, gate_scale, up_scale)
+    if isinstance(x, torch.Tensor) and x.dtype is E4M3:
+        x, ld = _matrix(x, "x", dtype=E4M3)
+        rows, cols = x.shape
+        w_gate, ld_gate = _columns_8(w_gate, "w_gate", cols, None, x)
+        hidden = w_gate.shape[1]
+        w_up, ld_up = _columns_8(w_up, "w_up", cols, hidden, x)
+        x_scale, gate_scale, up_scale = (_vector(_given(v, name), name, n, x, _F32) for v, name, n in
+                                         zip(scales, ("x_scale", "gate_scale", "up_scale"), (rows, hidden, hidden)))
+        out_dtype = out_dtype or torch.bfloat16
+        if out_dtype not in TYPES:
+            raise TypeError("out_dtype must be float32, bfloat16 or float16")
+    else:
+        x, ld = _matrix(x, "x")
+        rows, cols = x.shape
+        if scales != (None, None, None):
+            raise ValueError("scales go with 8-bit rows")
+        w_gate, ld_gate = _matrix(w_gate, "w_gate", cols, None, x.dtype, x)
+        hidden = w_gate.shape[1]
+        w_up, ld_up = _matrix(w_up, "w_up", cols, hidden, x.dtype, x)
+        if out_dtype not in (None, x.dtype):
+            raise TypeError("out_dtype must be x's type")
+        out_dtype = x.dtype
+    lib = _functions()
+    h = x.new_empty((rows, hidden), dtype=out_dtype)
+    _call(lib.ink_gated, x, x.data_ptr(), ld, _ptr(x_scale), w_gate.data_ptr(), ld_gate, w_up.data_ptr(), ld_up, _ptr(gate_scale), _ptr(up_scale),
+          rows, cols, hidden, _TYPES_8[x.dtype], TYPES[out_dtype], ACTS[act], h.data_ptr(), hidden)
+    return h
+
+
+def gated_backward(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dweights=True):
+    """(dx, dw_gate, dw_up) of gated, in x's type; None for what is not needed.  The projections are formed anew from x."""
+    x, ld = _matrix(x, "x")
+    rows, cols = x.shape
+    t = x.dtype
+    w_gate, ld_gate = _matrix(w_gate, "w_gate", cols, None, t, x)
+    hidden = w_gate.shape[1]
+    w_up, ld_up = _matrix(w_up, "w_up", cols, hidden, t, x)
+    dh, ld_dh = _matrix(dh, "dh", rows, hidden, t, x)
+    if act not in ACTS:
+        raise ValueError("act must be one of %s" % ", ".join(ACTS))
+    lib = _functions()
+    dx = x.new_empty((rows, cols)) if need_dx else None
+    dw_gate, dw_up = (x.new_empty((cols, hidden)), x.new_empty((cols, hidden))) if need_dweights else (None, None)
+    n_work = lib.ink_gated_backward_work(rows, cols, hidden, TYPES[t]) if need_dx or need_dweights else 0
+    work = x.new_empty(n_work, dtype=torch.uint8) if n_work else None
+    _call(lib.ink_gated_backward, x, dh.data_ptr(), ld_dh, x.data_ptr(), ld, w_gate.data_ptr(), ld_gate, w_up.data_ptr(), ld_up, rows, cols, hidden,
+          TYPES[t], ACTS[act], _ptr(dx), cols, _ptr(dw_gate), hidden, _ptr(dw_up), hidden, _ptr(work), n_work)
+    return dx, dw_gate, dw_up
+
+
+def adamw_moments(params, bits=32):
+    """Moments of AdamW at the start, one entry for each parameter: (m, v) of 32 bits or (m, m_scale, v, v_scale) of 8."""
+    if bits not in (8, 32):
+        raise ValueError("moments have 32 or 8 bits")
+    made = []
+    for p in params:
+        if bits == 32:
+            made.append(tuple(torch.zeros(p.shape, dtype=torch.float32, device=p.device) for _ in range(2)))
+        else:
+            scales = torch.zeros((2, -(-p.numel() // ADAMW_BLOCK)), dtype=torch.float32, device=p.device)
+            codes = [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(E4M3) for _ in range(2)]
+            made.append((codes[0], scales[0], codes[1], scales[1]))
+    return made
+
+
+def _held(t, name, like, dtypes):
+    """The address of a tensor that a step changes in place: of the parameter's shape and device, contiguous."""
+    if not isinstance(t, torch.Tensor) or t.shape != like.shape or t.device != like.device:
+        raise ValueError("%s must be a tensor of its parameter's shape, on its device" % name)
+    if t.dtype not in dtypes:
+        raise TypeError("%s has type %s, wanted %s" % (name, t.dtype, " or ".join(str(d) for d in dtypes)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous: the step changes it in place" % name)
+    return t.data_ptr()
+
+
+_PARAMS, _COPIES, _CODES, _ANY = (torch.float32, torch.bfloat16), (torch.bfloat16, torch.float16), (E4M3,), tuple(TYPES)
+
+
+def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=1.0, copies=None, seed=0):
+    """One step of AdamW over all of `params` (lists of tensors on one GPU, one entry for each), in place, in one launch for each 32 tensors.
+
+    params: float32 or bfloat16, contiguous.  grads: float32, bfloat16 or float16, None where there is none (that parameter is left as it
+    is).  moments: adamw_moments', all of one width.  copies: bfloat16 or float16 tensors that get the new float32 parameters (None, or a
+    list with None where there is none).  step: the step's number, from 1, or an int64 GPU tensor of one element that holds it.
+    grad_scale: a factor of every gradient, a number or a float32 GPU tensor of one element.  seed (64 bits): of the random numbers that round 8-bit
+    moments and bfloat16 parameters up or down in proportion; they depend on seed, step, place in the list and element alone."""
+    n = len(params)
+    if len(grads) != n or len(moments) != n or (copies is not None and len(copies) != n):
+        raise ValueError("params, grads, moments and copies must have one entry for each parameter")
+    given = [i for i in range(n) if grads[i] is not None]
+    if not given:
+        return
+    like = params[given[0]]
+    if not isinstance(like, torch.Tensor) or not like.is_cuda:
+        raise ValueError("params must be GPU tensors")
+    width = len(moments[given[0]])
+    if width not in (2, 4):
+        raise ValueError("moments must be adamw_moments': (m, v) or (m, m_scale, v, v_scale)")
+    groups, changed, kept, dev = {}, [], [], like.device
+    for i in given:
+        p, g, mom, copy = params[i], grads[i], moments[i], None if copies is None else copies[i]
+        at = _held(p, "a parameter", p, _PARAMS)
+        if p.device != dev:
+            raise ValueError("the parameters are on several devices")
+        if p.requires_grad and not p.is_leaf:
+            _unrecorded(p, "a parameter that is no leaf")
+        if g.shape != p.shape or g.device != dev or g.dtype not in TYPES:
+            raise ValueError("a gradient has shape %s and type %s on %s, its parameter shape %s on %s" % (tuple(g.shape), g.dtype, g.device, tuple(p.shape), dev))
+        if g.requires_grad:
+            _unrecorded(g, "a gradient")
+        if not g.is_contiguous():
+            g = g.contiguous()
+            kept.append(g)
+        size, c = p.numel(), 0
+        if len(mom) != width:
+            raise ValueError("moments of 32 and of 8 bits in one call")
+        if width == 2:
+            held = [at, _held(mom[0], "a first moment", p, _F32), _held(mom[1], "a second moment", p, _F32)]
+            m, v, ms, vs = held[1], held[2], 0, 0
+        else:
+            m, v, blocks = _held(mom[0], "a first moment", p, _CODES), _held(mom[2], "a second moment", p, _CODES), -(-size // ADAMW_BLOCK)
+            for s in (mom[1], mom[3]):
+                if s.dtype is not torch.float32 or s.device != dev or s.shape != (blocks,) or not s.is_contiguous():
+                    raise ValueError("a moment's scales must be a contiguous float32 tensor of shape [%d] on the parameter's device" % blocks)
+            ms, vs = mom[1].data_ptr(), mom[3].data_ptr()
+            held = [at, m, v, ms, vs]
+        if copy is not None:
+            if p.dtype is not torch.float32:
+                raise TypeError("a copy is of float32 parameters")
+            c = _held(copy, "a copy", p, _COPIES)
+            held.append(c)
+        if size:
+            changed += held
+        groups.setdefault((p.dtype, g.dtype, None if copy is None else copy.dtype), []).append((at, g.data_ptr(), c, m, v, ms, vs, size, i))
+    if len(set(changed)) != len(changed):
+        raise ValueError("a tensor that the step changes stands in the call twice")
+    step_at = scale_at = None
+    if isinstance(step, torch.Tensor):
+        if step.dtype is not torch.int64 or step.numel() != 1 or step.device != dev:
+            raise ValueError("step must be a number or an int64 tensor of one element on the parameters' device")
+        step_at, step = step.data_ptr(), 1
+    if isinstance(grad_scale, torch.Tensor):
+        if grad_scale.dtype is not torch.float32 or grad_scale.numel() != 1 or grad_scale.device != dev:
+            raise ValueError("grad_scale must be a number or a float32 tensor of one element on the parameters' device")
+        if grad_scale.requires_grad:
+            _unrecorded(grad_scale, "grad_scale")
+        scale_at, grad_scale = grad_scale.data_ptr(), 1.0
+    lib = _functions()
+    for (tp, tg, tc), entries in groups.items():
+        table = array.array("q", [x for e in entries for x in e])
+        _call(lib.ink_adamw, like, table.buffer_info()[0], len(entries), TYPES[tp], TYPES[tg], -1 if tc is None else TYPES[tc], 8 if width == 4 else 32, lr,
+              betas[0], betas[1], eps, weight_decay, step, step_at, grad_scale, scale_at, seed & 0xFFFFFFFFFFFFFFFF)
+    # what autograd has kept of these tensors is no longer what they hold
+    torch.autograd.graph.increment_version([t for i in given for t in (params[i], None if copies is None else copies[i])
+                                            if t is not None])

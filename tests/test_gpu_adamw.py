@@ -1,0 +1,292 @@
+"""The step of AdamW against its formula in 64 bits, with the same random numbers where numbers are rounded by chance.
+
+Tolerances: u = 2^-24 for each 32-bit operation.  A number that is rounded by chance may land on the other side only where the
+64-bit number lies within the 32-bit one's error of the border.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2309_11071_amd import head
+
+pytestmark = pytest.mark.gpu
+
+u = 2.0 ** -24
+F32, BF16, F16, E4M3 = torch.float32, torch.bfloat16, torch.float16, torch.float8_e4m3fn
+LR, B1, B2, EPS, DECAY = 3e-3, 0.9, 0.999, 1e-8, 0.1
+NEXT = 0x6A09E667
+
+
+def mix(x):
+    x = np.atleast_1d(np.asarray(x, dtype=np.uint64) & 0xFFFFFFFF).astype(np.uint32)
+    x = x ^ (x >> np.uint32(16))
+    x = x * np.uint32(0x9E3779B1)
+    x = x ^ (x >> np.uint32(15))
+    x = x * np.uint32(0xBB67AE85)
+    return x ^ (x >> np.uint32(16))
+
+
+def random_numbers(index, tensor, step, seed):
+    k = np.uint64(0)
+    for part in (tensor, step & 0xFFFFFFFF, step >> 32, seed & 0xFFFFFFFF, seed >> 32 & 0xFFFFFFFF):
+        k = mix(int(k) + part + NEXT)[0]
+    index = np.asarray(index, dtype=np.uint64)
+    keys = {int(h): mix(int(k) + int(h))[0] for h in np.unique(index >> np.uint64(32))}
+    key = np.array([keys[int(h)] for h in index >> np.uint64(32)], dtype=np.uint32) if len(keys) > 1 else next(iter(keys.values()))
+    first = mix((index.astype(np.uint32) ^ key).astype(np.uint64))
+    return first, mix(first.astype(np.uint64) + NEXT)
+
+
+def grid(a, least):
+    """Distance of the numbers of 3 bits behind the first around a, subnormal below 2^least."""
+    return np.ldexp(1.0, np.maximum(np.frexp(a)[1] - 1, least) - 3)
+
+
+def blocks(x):
+    n = -(-x.size // head.ADAMW_BLOCK)
+    return np.pad(x, (0, n * head.ADAMW_BLOCK - x.size)).reshape(n, -1)
+
+
+def check_chance(got, exact, step, bits, numbers, err, what):
+    """got is exact rounded down to a multiple of step, or up where numbers / 2^bits and the rest pass 1; err: of exact, in steps."""
+    at = np.abs(exact) / step
+    want = np.floor(np.floor(at * 2.0 ** bits) / 2.0 ** bits + numbers / 2.0 ** bits)
+    have = np.abs(got) / step
+    off = have != want
+    edge = at + numbers / 2.0 ** bits
+    near = np.abs(edge - np.round(edge)) <= err + 2.0 ** -bits
+    assert (np.abs(have - want)[off] <= 1).all() and near[off].all(), (what, int((off & ~near).sum()))
+    assert off.mean() <= 0.01 or got.size < 1000, what
+
+
+def step_ref(p, g, m, v, t, scale):
+    p, g, m, v = (a.astype(np.float64) for a in (p, g, m, v))
+    g = g * scale
+    e_m = 4 * u * (B1 * np.abs(m) + (1 - B1) * np.abs(g))
+    m = B1 * m + (1 - B1) * g
+    v = B2 * v + (1 - B2) * g * g
+    root = np.sqrt(v)
+    by = LR / (1 - B1 ** t) / (root / np.sqrt(1 - B2 ** t) + EPS)
+    p2 = p * (1 - LR * DECAY) - by * m
+    return p2, m, v, root, by * e_m + 16 * u * np.abs(by * m) + 3 * u * np.abs(p), e_m
+
+
+def state(n, dtype, gtype, ctype, bits, gen, used=True):
+    p = (torch.randn(n, generator=gen) * 0.05).to(dtype)
+    g = (torch.randn(n, generator=gen) * torch.exp(torch.randn(n, generator=gen)) * 1e-2).to(gtype)
+    mom = head.adamw_moments([p.cuda()], bits)[0]
+    if used:
+        m, r = torch.randn(n, generator=gen) * 1e-2, torch.rand(n, generator=gen) * 2e-2
+        if bits == 32:
+            mom[0].copy_(m), mom[1].copy_(r * r)
+        else:
+            for k, x in ((0, m), (2, r)):
+                scale = torch.from_numpy(blocks(x.numpy())).abs().amax(1) / 448 if n else torch.zeros(0)
+                mom[k].copy_((x / scale.clamp(min=1e-30).repeat_interleave(128)[:n]).to(E4M3)), mom[k + 1].copy_(scale)
+    return p.cuda(), g.cuda(), mom, None if ctype is None else torch.zeros(n, dtype=ctype, device="cuda")
+
+
+def numbers_of(mom, n):
+    """m and v as 64-bit numbers."""
+    if len(mom) == 2:
+        return mom[0].double().cpu().numpy(), mom[1].double().cpu().numpy()
+    m, sm, v, sv = (x.float().cpu().numpy().astype(np.float64) for x in mom)
+    each = lambda s: np.repeat(s, 128)[:n]                        # noqa: E731
+    return (m * each(sm)).astype(np.float32).astype(np.float64), (v * each(sv)).astype(np.float32).astype(np.float64) ** 2
+
+
+def check_step(entries, step, seed, scale=1.0, places=None, step_arg=None, scale_arg=None):
+    """One call over entries (param, grad, moments, copy), checked element by element."""
+    n_of = [e[0].numel() for e in entries]
+    before = [(p.double().cpu().numpy().reshape(-1), g.double().cpu().numpy().reshape(-1), *numbers_of([x.reshape(-1) for x in mom], n)) for (p, g, mom, _), n in zip(entries, n_of)]
+    copies = [e[3] for e in entries]
+    head.adamw([e[0] for e in entries], [e[1] for e in entries], [e[2] for e in entries], step if step_arg is None else step_arg, lr=LR, betas=(B1, B2), eps=EPS, weight_decay=DECAY,
+               grad_scale=scale if scale_arg is None else scale_arg, copies=copies if any(c is not None for c in copies) else None, seed=seed)
+    for i, ((p, g, mom, copy), (p0, g0, m0, v0), n) in enumerate(zip(entries, before, n_of)):
+        want, m, v, root, e_p, e_m = step_ref(p0, g0, m0, v0, step, scale)
+        first, second = random_numbers(np.arange(n), i if places is None else places[i], step, seed)
+        got = p.double().cpu().numpy().reshape(-1)
+        if p.dtype is BF16:
+            s = np.ldexp(1.0, np.maximum(np.frexp(want)[1] - 1, -126) - 7)
+            check_chance(got, want, s, 16, (first >> 20) + ((second >> 20 & 15) << 12), e_p / s, "param")
+        else:
+            assert (np.abs(got - want) <= e_p + u * np.abs(want)).all(), "param"
+            if copy is not None:
+                assert torch.equal(copy.reshape(-1), p.reshape(-1).to(copy.dtype)), "copy"
+        if len(mom) == 2:
+            assert (np.abs(mom[0].double().cpu().numpy().reshape(-1) - m) <= e_m + u * np.abs(m)).all(), "m"
+            assert (np.abs(mom[1].double().cpu().numpy().reshape(-1) - v) <= 6 * u * v).all(), "v"
+            continue
+        for x, e, codes, scales, numbers, root_too in ((m, e_m, mom[0], mom[1], first, False), (root, 6 * u * root, mom[2], mom[3], second, True)):
+            x, e = blocks(x), blocks(e)
+            top = np.abs(x).max(1)
+            s = scales.double().cpu().numpy()
+            assert (np.abs(s - top / 448) <= (e.max(1) + 2 * u * top) / 448 * 1.001).all(), "scale"
+            at = x / np.where(s > 0, s, 1)[:, None]
+            err = np.abs(e / np.where(s > 0, s, 1)[:, None]) + 4 * u * np.abs(at)
+            q = blocks(codes.float().cpu().numpy().astype(np.float64).reshape(-1))
+            st, numbers = grid(at, -6), blocks(numbers.astype(np.float64) % 2 ** 20)
+            if root_too:
+                assert (q.reshape(-1)[:n][root > 0] >= 2.0 ** -9).all(), "a root that is not 0 stays so"
+                low = (q == 2.0 ** -9) & (at < 2.0 ** -9)
+                q = np.where(low, np.floor(at / st + numbers / 2 ** 20) * st, q)
+            top_one = np.abs(at) >= 448 - err                     # no number is larger than the largest
+            q, at = np.where(top_one, 448.0, np.abs(q)), np.where(top_one, 448.0, at)
+            check_chance(q, at, st, 20, numbers, err / st, "codes")
+            assert (np.signbit(codes.float().cpu().numpy().reshape(-1)[:n]) <= np.signbit(x.reshape(-1)[:n])).all() or not root_too
+
+
+SIZES = [1, 2, 7, 8, 9, 127, 128, 129, 1000, 2047, 2048, 2049, 5000]
+KINDS = [(F32, F32, None), (F32, BF16, BF16), (F32, F16, F16), (F32, F32, BF16), (F32, BF16, F16), (F32, BF16, None), (BF16, BF16, None), (BF16, F32, None), (BF16, F16, None)]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("kind", range(len(KINDS)))
+def test_a_step_over_many_tensors(kind, bits):
+    gen = torch.Generator().manual_seed(kind * 7 + bits)
+    check_step([state(n, *KINDS[kind], bits, gen) for n in SIZES * 3], 17, 12345)           # 39 tensors: two launches
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("step,seed", [(1, 0), (2, 2 ** 64 - 1), (100_000, 5), (2 ** 33 + 1, 2 ** 40)])
+def test_steps_and_seeds(step, seed, bits):
+    gen = torch.Generator().manual_seed(step % 1000 + bits)
+    check_step([state(n, F32, F32, None, bits, gen, used=step > 1) for n in (300, 5000)], step, seed)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_views_that_start_anywhere(bits):
+    """Parameters, gradients, copies and moments as pieces of larger buffers, at any element's alignment."""
+    gen = torch.Generator().manual_seed(3)
+    made = []
+    for n, off in ((500, 1), (1201, 3), (64, 5)):
+        p, g, mom, c = state(n, F32, BF16, BF16, bits, gen)
+
+        def moved(x):
+            flat = torch.zeros(x.numel() + 9, dtype=x.dtype if x.dtype is not E4M3 else torch.uint8, device="cuda")
+            flat = flat.view(x.dtype)
+            v = flat[off:off + x.numel()]
+            v.copy_(x)
+            return v
+        made.append((moved(p), moved(g), tuple(moved(x) for x in mom), moved(c)))
+    check_step(made, 9, 77)
+
+
+def test_a_number_of_several_shapes_types_and_gaps():
+    """Groups of types in one call, shapes of several dimensions, a parameter without a gradient, one without elements."""
+    gen = torch.Generator().manual_seed(5)
+    a, b, c = state(600, F32, F32, None, 8, gen), state(700, F32, BF16, F16, 8, gen), state(800, BF16, BF16, None, 8, gen)
+    empty = (torch.empty(0, device="cuda"), torch.empty(0, device="cuda"), head.adamw_moments([torch.empty(0, device="cuda")], 8)[0], None)
+    shaped = [tuple(x.view(s) if isinstance(x, torch.Tensor) else x for x in e[:2]) + (tuple(x.view(s) if x.numel() == e[0].numel() else x for x in e[2]), None if e[3] is None else e[3].view(s))
+              for e, s in ((a, (20, 30)), (b, (7, 10, 10)), (c, (800,)))]
+    idle = state(100, F32, F32, None, 8, gen)
+    was = [x.clone() for x in (idle[0], *idle[2])]
+    entries = [shaped[0], (idle[0], None, idle[2], None), shaped[1], empty, shaped[2]]
+    before = [tuple(x.clone() if isinstance(x, torch.Tensor) else x for x in e[:2]) + (tuple(x.clone() for x in e[2]), None if e[3] is None else e[3].clone()) for e in shaped]
+    head.adamw([e[0] for e in entries], [e[1] for e in entries], [e[2] for e in entries], 3, lr=LR, betas=(B1, B2), eps=EPS, weight_decay=DECAY, copies=[e[3] for e in entries], seed=4)
+    for x, y in zip((idle[0], *idle[2]), was):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), "no gradient: left as it was"
+    for place, got, old in zip((0, 2, 4), shaped, before):
+        alone = [torch.empty(0, device="cuda")] * 5
+        alone[place] = old[0]
+        grads = [None] * 5
+        grads[place] = old[1]
+        head.adamw(alone, grads, [empty[2]] * place + [old[2]] + [empty[2]] * (4 - place), 3, lr=LR, betas=(B1, B2), eps=EPS, weight_decay=DECAY,
+                   copies=[None] * place + [old[3]] + [None] * (4 - place), seed=4)
+        for x, y in zip((got[0], *got[2]), (old[0], *old[2])):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), "a tensor's step does not depend on the others"
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_step_and_scale_on_the_device(bits):
+    gen = torch.Generator().manual_seed(8)
+    check_step([state(n, F32, F16, F16, bits, gen) for n in (300, 5000)], 41, 6, scale=1 / 1024,
+               step_arg=torch.tensor(41, device="cuda"), scale_arg=torch.tensor([1 / 1024], device="cuda"))
+    check_step([state(n, F32, F16, F16, bits, gen) for n in (300, 5000)], 1, 6, scale=0.5, step_arg=torch.tensor([-7], device="cuda"))
+
+
+@pytest.mark.parametrize("dtype,bits", [(F32, 8), (BF16, 32), (BF16, 8)])
+def test_a_captured_step_counts_on(dtype, bits):
+    gen = torch.Generator().manual_seed(9)
+    e = state(3000, dtype, F32, None, bits, gen)
+    twin = [x.clone() for x in (e[0], *e[2])]
+    at = torch.tensor(4, device="cuda")
+
+    def call(p, mom, step):
+        head.adamw([p], [e[1]], [mom], step, lr=LR, seed=2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        keep = [x.clone() for x in (e[0], *e[2])]
+        call(e[0], e[2], at)
+        for x, y in zip((e[0], *e[2]), keep):
+            x.copy_(y)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        at.add_(1)
+        call(e[0], e[2], at)
+    for step in (5, 6, 7):
+        graph.replay()
+        torch.cuda.synchronize()
+        call(twin[0], tuple(twin[1:]), step)                      # eager work between the replays
+        for x, y in zip((e[0], *e[2]), twin):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), step
+
+
+def test_rounding_by_chance_keeps_the_expectation():
+    """An average that moves by less than half a step of 8 bits still moves: of n elements rounded independently the mean is off by at most
+    6 standard deviations, each at most half a step / sqrt(n); the same gradient for 400 steps of beta2 = 0.999."""
+    n = 128 * 512
+    p = torch.zeros(n, device="cuda")
+    g = torch.full((n,), 1e-3, device="cuda")
+    g[::128] = 1.0                                                # one element sets each block's scale
+    mom = head.adamw_moments([p], 8)
+    for t in range(1, 401):
+        head.adamw([p], [g], mom, t, lr=0.0, weight_decay=0.0, seed=11)
+    # Every small root is 1e-3 of its block's largest, 0.448 in units of the scale, between the numbers 14 / 32 and 15 / 32: s = 1 / 32, 0.07 of it.
+    # Rounding keeps the root's expectation; sqrt(b v^2 + c) is convex, so the mean does not fall below the exact root.  The
+    # second moment grows by the rounding's variance: a step moves the root by at most 1 / t of s, so the variance is at most s^2 / t, and over 400
+    # steps the sum at most 0.07^2 (1 - beta2) 400 g^2 against 0.33 g^2: 0.6 %, 0.3 % of the root.  Sampling: 6 * 0.07 / sqrt(65024) = 0.17 %.
+    root = (mom[0][2].float() * mom[0][3].repeat_interleave(128)).view(-1, 128)[:, 1:].double()
+    want = 1e-3 * (1 - 0.999 ** 400) ** 0.5
+    assert 0.998 * want <= float(root.mean()) <= 1.005 * want, (float(root.mean()), want)
+    # the first moment's errors die out with 0.9 a step: their variance is at most (s / 2)^2 / (1 - 0.81)
+    m = (mom[0][0].float() * mom[0][1].repeat_interleave(128)).view(-1, 128)[:, 1:].double()
+    assert abs(float(m.mean()) - 1e-3) <= 6 * 0.07e-3 * (0.25 / 0.19) ** 0.5 / m.numel() ** 0.5
+    q = torch.full((n,), 1.0, dtype=BF16, device="cuda")          # 1e-4 a step is a 39th of half a step of bfloat16 below 1
+    mom = head.adamw_moments([q], 32)
+    for t in range(1, 101):
+        head.adamw([q], [torch.ones(n, device="cuda")], mom, t, lr=1e-4, weight_decay=0.0, seed=3)
+    assert abs(float(q.double().mean()) - 0.99) <= 6 * 2.0 ** -9 * 10 / n ** 0.5
+
+
+def test_gradients_that_are_no_numbers():
+    for bits in (32, 8):
+        e = state(1000, F32, F32, None, bits, torch.Generator().manual_seed(1))
+        e[1][300], e[1][700] = float("nan"), float("inf")
+        head.adamw([e[0]], [e[1]], [e[2]], 2)
+        bad = torch.zeros(1000, dtype=torch.bool)
+        bad[300] = bad[700] = True
+        assert torch.equal(torch.isfinite(e[0]).cpu(), ~bad), "the parameters: these elements alone"
+        if bits == 8:
+            assert torch.equal(torch.isnan(e[2][1]).cpu().nonzero()[:, 0], torch.tensor([2, 5])), "the moments: their blocks"
+
+
+def test_more_than_2_32_elements():
+    n = 2 ** 32 + 5000
+    p = torch.full((n,), 0.5, dtype=BF16, device="cuda")
+    g = torch.full((n,), 0.01, dtype=BF16, device="cuda")
+    mom = head.adamw_moments([p], 8)
+    head.adamw([p], [g], mom, 1, lr=LR, betas=(B1, B2), eps=EPS, weight_decay=DECAY, seed=21)
+    for at in (0, 2 ** 31 - 100, 2 ** 32 - 300, 2 ** 32, n - 200):
+        index = np.arange(at, at + 200)
+        first, second = random_numbers(index, 0, 1, 21)
+        g0 = np.float64(float(g[0]))
+        want, m, v, root, e_p, e_m = step_ref(np.full(200, 0.5), np.full(200, g0), np.zeros(200), np.zeros(200), 1, 1.0)
+        s = np.full(200, 2.0 ** -9)
+        check_chance(p[at:at + 200].double().cpu().numpy(), want, s, 16, (first >> 20) + ((second >> 20 & 15) << 12), e_p / s, "param")
+        assert (mom[0][0][at:at + 200].float() == 448).all()
+    assert abs(float(mom[0][1][-1]) * 448 - (1 - B1) * g0) <= 4 * u * g0
+    del p, g, mom
+    torch.cuda.empty_cache()
