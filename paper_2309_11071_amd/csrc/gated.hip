@@ -104,27 +104,42 @@ template <class T> __device__ __forceinline__ typename Frag<T>::V deep_frag(cons
   }
 }
 
-// h of four neighbouring columns
-__device__ __forceinline__ void gate4(float g[4], const float u[4], int act) {
-  activate_all<4>(g, act);
+// What the lanes of a wave have put into LDS is there for its other lanes: a wave's accesses are in order, so this holds the compiler alone.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// h of a lane's elements in place of g: one decision for all of them, whose exponentials are then under way side by side
+template <int N> __device__ __forceinline__ void gate_all(float g[N], const float u[N], int act) {
+  activate_all<N>(g, act);
 #pragma unroll
-  for (int j = 0; j < 4; j++) g[j] *= u[j];
+  for (int j = 0; j < N; j++) g[j] *= u[j];
+}
+// value and slope of an activation, which share their exponential
+__device__ __forceinline__ float activate_both(float z, float &slope, int act) {
+  if (act == INK_ACT_RELU) { slope = z > 0.f ? 1.f : z <= 0.f ? 0.f : z; return z < 0.f ? 0.f : z; }
+  if (act == INK_ACT_GELU) { float pdf; const float cdf = normal_cdf(z, pdf); slope = fmaf(z, pdf, cdf); return z * cdf; }
+  if (act == INK_ACT_SILU) { const float s = sigmoid(z); slope = s * fmaf(z, 1.f - s, 1.f); return z * s; }
+  slope = 1.f;
+  return z;
 }
 // dg and du in place of g and u
-__device__ __forceinline__ void gate4_grad(float g[4], float u[4], const float dh[4], int act) {
-  float du[4];
+template <int N, int ACT> __device__ __forceinline__ void gate_grad_of(float g[N], float u[N], const float dh[N]) {
 #pragma unroll
-  for (int j = 0; j < 4; j++) {
-    du[j] = g[j];
-    u[j] *= dh[j];
+  for (int j = 0; j < N; j++) {
+    float slope;
+    const float a = activate_both(g[j], slope, ACT);
+    g[j] = dh[j] * u[j] * slope;
+    u[j] = dh[j] * a;
   }
-  activate_all<4>(du, act);
-  if (act != INK_ACT_NONE) scale_by_slope<4>(u, g, act);
-#pragma unroll
-  for (int j = 0; j < 4; j++) {
-    g[j] = u[j];
-    u[j] = du[j] * dh[j];
-  }
+}
+template <int N> __device__ __forceinline__ void gate_grad_all(float g[N], float u[N], const float dh[N], int act) {
+  if (act == INK_ACT_SILU) gate_grad_of<N, INK_ACT_SILU>(g, u, dh);
+  else if (act == INK_ACT_GELU) gate_grad_of<N, INK_ACT_GELU>(g, u, dh);
+  else if (act == INK_ACT_RELU) gate_grad_of<N, INK_ACT_RELU>(g, u, dh);
+  else gate_grad_of<N, INK_ACT_NONE>(g, u, dh);
 }
 
 // ------------------------------------------------------------------------------------ tiles
@@ -238,33 +253,32 @@ __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
     const int row = (wm * RB + i) * 32 + l % 32;
     float scale = 1.f;
     if constexpr (!DEEP) scale = a.x_scale[min(m0 + row, a.rows - 1)];
+    float gv[16], uv[16];
+    TO *at = reinterpret_cast<TO *>(s_mem + row * PO) + wn * 32 + 4 * half;      // four neighbouring columns, four times 8 apart
 #pragma unroll
-    for (int e = 0; e < 4; e++) {
-      const int c = wn * 32 + 8 * e + 4 * half;
-      float gv[4], uv[4];
-#pragma unroll
-      for (int j = 0; j < 4; j++) { gv[j] = g[i][4 * e + j]; uv[j] = u[i][4 * e + j]; }
+    for (int e = 0; e < 16; e++) {
+      gv[e] = g[i][e];
+      uv[e] = u[i][e];
       if constexpr (!DEEP) {
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const int n = min(n0 + c + j, a.hidden - 1);
-          gv[j] *= scale * a.gate_scale[n];
-          uv[j] *= scale * a.up_scale[n];
-        }
+        const int n = min(n0 + wn * 32 + 8 * (e / 4) + 4 * half + e % 4, a.hidden - 1);
+        gv[e] *= scale * a.gate_scale[n];
+        uv[e] *= scale * a.up_scale[n];
       }
-      TO *at = reinterpret_cast<TO *>(s_mem + row * PO) + c;
-      if constexpr (GRAD) {
-        float dh[4];
-        load_pack<TO, 4>(at, dh);
-        gate4_grad(gv, uv, dh, a.act);
-        if (n0 + kTileHidden > a.hidden)       // behind the last column the products that follow find zeros, whatever x holds
-#pragma unroll
-          for (int j = 0; j < 4; j++)
-            if (n0 + c + j >= a.hidden) gv[j] = uv[j] = 0.f;
-        store_pack<TO, 4>(reinterpret_cast<TO *>(s_mem + (BM + row) * PO) + c, uv);
-      } else gate4(gv, uv, a.act);
-      store_pack<TO, 4>(at, gv);
     }
+    if constexpr (GRAD) {
+      float dh[16];
+#pragma unroll
+      for (int e = 0; e < 4; e++) load_pack<TO, 4>(at + 8 * e, dh + 4 * e);
+      gate_grad_all<16>(gv, uv, dh, a.act);
+      if (n0 + kTileHidden > a.hidden)         // behind the last column the products that follow find zeros, whatever x holds
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+          if (n0 + wn * 32 + 8 * (e / 4) + 4 * half + e % 4 >= a.hidden) gv[e] = uv[e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; e++) store_pack<TO, 4>(at + BM * PO / (int)sizeof(TO) + 8 * e, uv + 4 * e);
+    } else gate_all<16>(gv, uv, a.act);
+#pragma unroll
+    for (int e = 0; e < 4; e++) store_pack<TO, 4>(at + 8 * e, gv + 4 * e);
   }
   __syncthreads();
   if constexpr (GRAD) {
@@ -290,6 +304,254 @@ __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
       }
     }
   }
+}
+
+// ------------------------------------------------------------------------------------ many rows
+// Rows in a stream past weights in registers: a wave has the fragments of 32 columns of Wg and of Wu over the whole depth (KS steps) for good, a
+// workgroup WN waves side by side and WM below each other.  It takes 32 RB WM rows at a time; all threads load them side by side, a
+// tile ahead, into one of two buffers in LDS, from where every wave reads the fragments of its rows: one barrier a tile.  The results
+// turn in LDS that is the wave's own, from four columns a lane to 64 bytes of a row side by side, so no wave waits for another's activations.  The
+// next tile's rows go into LDS before this tile's results are stored: memory answers in order, so a wait for rows asked for is one for all
+// stores before them, and those of the tile before have had the products' time (2.45M x 128 x 344 bf16: 812 us with the stores first).
+struct StreamPlan { int groups, row_groups; };               // workgroups side by side, and below each other
+template <class T, int KS, int WM> constexpr int stream_blocks() { return WM > 1 || KS * kTypeStep<T> * (int)sizeof(T) > 256 || sizeof(T) == 2 ? 1 : 2; }
+template <class T, class TO, int KS, int WN, int WM, int PER, bool GRAD>
+__global__ __launch_bounds__(kWave * WN * WM, PER) void k_gated_stream(GatedArgs a, StreamPlan plan) {
+  typedef typename Frag<T>::V V;
+  constexpr bool DEEP = sizeof(T) != 1;
+  constexpr int THREADS = kWave * WN * WM, RB = stream_blocks<T, KS, WM>(), MR = 32 * RB * WM;
+  constexpr int KB = KS * kTypeStep<T> * (int)sizeof(T), P = KB + 16;        // bytes of a row, and between rows in LDS
+  constexpr int PE = 16 / sizeof(T), ROWS = THREADS / (KB / 16), NL = (MR + ROWS - 1) / ROWS;     // a thread's piece has one place in rows ROWS apart
+  constexpr int OE = 16 / sizeof(TO), OP = 32 / OE, OROWS = kWave / OP, NO = 32 / OROWS;          // a wave stores OROWS rows of 32 columns at once
+  constexpr int PO = 32 * (int)sizeof(TO) + 16, OWN = 32 * PO * (GRAD ? 2 : 1);                 // a wave's 32 rows of 32 results
+  constexpr int PWT = 32 * (int)sizeof(T) + 16;              // a step of W on its way to the registers
+  static_assert(THREADS % (KB / 16) == 0, "whole rows of pieces");
+  static_assert(!DEEP || 2 * kTypeStep<T> * PWT <= OWN, "a step of W fits a wave's own memory");
+  extern __shared__ __align__(16) char s_mem[];
+  char *s_x = s_mem;
+  const int tid = threadIdx.x, l = lane_id(), half = l / 32, wave = __builtin_amdgcn_readfirstlane(tid / kWave), wn = wave % WN, wm = wave / WN;
+  char *s_own = s_mem + 2 * MR * P + wave * OWN;
+  // workgroups go to the eight chiplets in turn: those that read the same rows are eight apart
+  const int id = blockIdx.x / 8, group = id % plan.groups;
+  const int64_t first = (int64_t)(id / plan.groups) * 8 + blockIdx.x % 8, tiles = (a.rows + MR - 1) / MR;
+  // A wave that the last column cuts takes the last 32 columns instead, some of which the wave before it has too: the same numbers.  (dg and du
+  // are stored up to whole tiles, with zeros.)
+  const int n_first = (group * WN + wn) * 32, n0 = GRAD || n_first >= a.hidden ? n_first : max(0, min(n_first, a.hidden - 32));
+  // Addresses are a uniform base and 32 bits a lane.  A piece that the row's end cuts is loaded from its last 16 bytes and moved down, one
+  // past it is zero; of the last tile the last row stands in for those past the end.
+  const int row = tid / (KB / 16), col = tid % (KB / 16) * PE;
+  const uint32_t x_at = (__umul24(row, (uint32_t)a.ld_x) + min(col, a.cols - PE)) * (uint32_t)sizeof(T);
+  Piece x[NL];
+  auto fetch = [&](int64_t t) {
+    const char *base = reinterpret_cast<const char *>(static_cast<const T *>(a.x) + t * MR * a.ld_x);
+    const int left = (int)min(a.rows - t * MR, (int64_t)MR);
+#pragma unroll
+    for (int j = 0; j < NL; j++) {
+      if (MR % ROWS && j == NL - 1 && row + j * ROWS >= MR) continue;
+      uint32_t at = x_at;
+      if (left < MR) at -= max(0, row + j * ROWS - left + 1) * (uint32_t)a.ld_x * (uint32_t)sizeof(T);
+      x[j] = (Piece)*reinterpret_cast<const PieceAny *>(base + (int64_t)j * ROWS * a.ld_x * (int)sizeof(T) + (int64_t)(int32_t)at);
+    }
+  };
+  auto put = [&](int buffer) {
+#pragma unroll
+    for (int j = 0; j < NL; j++) {
+      if (MR % ROWS && j == NL - 1 && row + j * ROWS >= MR) continue;
+      if (col + PE > a.cols) x[j] = col < a.cols ? move_down(x[j], col + PE - a.cols, sizeof(T)) : Piece{};
+      *reinterpret_cast<Piece *>(s_x + (buffer * MR + j * ROWS + row) * P + tid % (KB / 16) * 16) = x[j];
+    }
+  };
+  int64_t t = first;
+  if (t < tiles) fetch(t);
+  V w[2][KS];
+  if constexpr (DEEP) {
+    constexpr int PR = 32 / PE;              // pieces of a step's row: 64 lanes take a whole step
+    const int k = l / PR, n = n0 + l % PR * PE;
+    Piece q[2][KS];
+#pragma unroll
+    for (int s = 0; s < KS; s++)
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        const int kk = s * kTypeStep<T> + k;
+        const T *from = static_cast<const T *>(h ? a.up : a.gate) + (int64_t)min(kk, a.cols - 1) * (h ? a.ld_up : a.ld_gate);
+        q[h][s] = (Piece)*reinterpret_cast<const PieceAny *>(from + min(n, a.hidden - PE));
+        if (kk >= a.cols || n >= a.hidden) q[h][s] = Piece{};
+        else if (n + PE > a.hidden) q[h][s] = move_down(q[h][s], n + PE - a.hidden, sizeof(T));
+      }
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+#pragma unroll
+      for (int h = 0; h < 2; h++) *reinterpret_cast<Piece *>(s_own + h * kTypeStep<T> * PWT + k * PWT + l % PR * 16) = q[h][s];
+      wave_order();
+#pragma unroll
+      for (int h = 0; h < 2; h++) w[h][s] = deep_frag<T>(s_own + h * kTypeStep<T> * PWT, PWT, 0, 0);
+      wave_order();
+    }
+  } else {
+    const int n = n0 + l % 32;
+#pragma unroll
+    for (int s = 0; s < KS; s++)
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        Piece q[2];
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+          const int k = s * kTypeStep<T> + half * 32 + 16 * j;
+          const T *from = static_cast<const T *>(h ? a.up : a.gate) + (int64_t)min(n, a.hidden - 1) * (h ? a.ld_up : a.ld_gate);
+          q[j] = (Piece)*reinterpret_cast<const PieceAny *>(from + min(k, a.cols - PE));
+          if (k >= a.cols || n >= a.hidden) q[j] = Piece{};
+          else if (k + PE > a.cols) q[j] = move_down(q[j], k + PE - a.cols, sizeof(T));
+        }
+        w[h][s] = __builtin_shufflevector(q[0], q[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+  }
+  F4 *s_scale = reinterpret_cast<F4 *>(s_mem + 2 * MR * P + WN * WM * OWN) + wave * 16;      // 8-bit weights: scales of this wave's columns
+  if constexpr (!DEEP) {
+    reinterpret_cast<float *>(s_scale)[l] = (l < 32 ? a.gate_scale : a.up_scale)[min(n0 + l % 32, a.hidden - 1)];
+    wave_order();
+  }
+  const bool whole = n0 + 32 <= a.hidden;
+  const int orow = l / OP, ocol = l % OP * OE;               // this lane's piece of the results: rows OROWS apart
+  const uint32_t o_at = (__umul24(orow, (uint32_t)a.ld_out) + ocol) * (uint32_t)sizeof(TO);
+  const uint32_t d_at = GRAD ? (__umul24(orow, (uint32_t)a.ld_dh) + max(0, min(n0 + ocol, a.hidden - OE))) * (uint32_t)sizeof(TO) : 0;
+  if (t >= tiles) return;                    // the whole workgroup
+  const int64_t last = t + (tiles - 1 - t) / plan.row_groups * plan.row_groups;
+  // What else a tile reads, a tile ahead: dh of the wave's rows (64 bytes or more side by side), scales of its 8-bit rows.
+  constexpr int ND = 32 / OROWS;
+  Piece dhp[GRAD ? RB * ND : 1];
+  float scale[DEEP ? 1 : RB];
+  auto fetch_more = [&](int64_t t, auto plain) {
+#pragma unroll
+    for (int rb = 0; rb < RB; rb++) {
+      const int64_t my_row = t * MR + (wm * RB + rb) * 32;
+      if constexpr (!DEEP) scale[rb] = a.x_scale[min(my_row + l % 32, a.rows - 1)];
+      if constexpr (GRAD)
+#pragma unroll
+        for (int j = 0; j < ND; j++) {
+          if constexpr (plain()) {
+            const char *base = reinterpret_cast<const char *>(static_cast<const TO *>(a.dh) + (my_row + j * OROWS) * a.ld_dh);
+            dhp[rb * ND + j] = (Piece)*reinterpret_cast<const PieceAny *>(base + d_at);
+          } else {
+            const int64_t r = min(my_row + j * OROWS + orow, a.rows - 1);
+            dhp[rb * ND + j] = (Piece)*reinterpret_cast<const PieceAny *>(static_cast<const TO *>(a.dh) + r * a.ld_dh + min(n0 + ocol, a.hidden - OE));
+          }
+        }
+    }
+  };
+  // One tile.  PLAIN: not this workgroup's last one, and all 32 columns there: the stores are then under no condition, and the wait for the next
+  // tile's rows is not one for them (one wave of a launch with a condition on its stores: 2.45M x 128 x 344 bf16 940 us).
+  auto tile = [&](int64_t t, int buffer, auto plain) {
+    constexpr bool PLAIN = plain();
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < RB; rb++) {
+      const int64_t my_row = t * MR + (wm * RB + rb) * 32;
+      f32x16 g = f32x16{}, u = f32x16{};
+      const char *xs = s_x + (buffer * MR + (wm * RB + rb) * 32) * P;
+      // fragments are asked for AHEAD steps before their products: left alone, the compiler asks for one at a time and waits for it
+      constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;
+      V f[AHEAD];
+#pragma unroll
+      for (int s = 0; s < AHEAD; s++) f[s] = rows_frag<T>(xs, P, s);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < KS; s++) {
+        const V xf = f[s % AHEAD];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            g = __builtin_amdgcn_mfma_f32_32x32x2f32(w[0][s][j], xf[j], g, 0, 0, 0);
+            u = __builtin_amdgcn_mfma_f32_32x32x2f32(w[1][s][j], xf[j], u, 0, 0, 0);
+          }
+        } else {
+          g = mma(w[0][s], xf, g);
+          u = mma(w[1][s], xf, u);
+        }
+        if (s + AHEAD < KS) f[s % AHEAD] = rows_frag<T>(xs, P, s + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (GRAD) {
+#pragma unroll
+        for (int j = 0; j < ND; j++) {
+          Piece &d = dhp[rb * ND + j];
+          if (!whole && n0 + ocol + OE > a.hidden) d = n0 + ocol < a.hidden ? move_down(d, n0 + ocol + OE - a.hidden, sizeof(TO)) : Piece{};
+          *reinterpret_cast<Piece *>(s_own + (orow + j * OROWS) * PO + l % OP * 16) = d;
+        }
+        wave_order();
+      }
+      constexpr int N = GRAD ? 8 : 16;         // elements at a time
+#pragma unroll
+      for (int q = 0; q < 16 / N; q++) {
+        float gv[N], uv[N];
+        TO *at = reinterpret_cast<TO *>(s_own + (l % 32) * PO) + 16 * q + 4 * half;          // four neighbouring columns at a time, 8 apart
+#pragma unroll
+        for (int e = 0; e < N; e++) {
+          gv[e] = g[8 * q + e];
+          uv[e] = u[8 * q + e];
+          if constexpr (!DEEP) {
+            gv[e] *= scale[rb] * s_scale[4 * q + 2 * (e / 4) + half][e % 4];
+            uv[e] *= scale[rb] * s_scale[8 + 4 * q + 2 * (e / 4) + half][e % 4];
+          }
+        }
+        if constexpr (GRAD) {
+          float dh[8];
+#pragma unroll
+          for (int e = 0; e < 2; e++) load_pack<TO, 4>(at + 8 * e, dh + 4 * e);
+          gate_grad_all<8>(gv, uv, dh, a.act);
+          if (!whole)                          // behind the last column the products that follow find zeros, whatever x holds
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              if (n0 + 16 * q + 8 * (e / 4) + 4 * half + e % 4 >= a.hidden) gv[e] = uv[e] = 0.f;
+#pragma unroll
+          for (int e = 0; e < 2; e++) store_pack<TO, 4>(at + 32 * PO / (int)sizeof(TO) + 8 * e, uv + 4 * e);
+        } else gate_all<N>(gv, uv, a.act);
+#pragma unroll
+        for (int e = 0; e < N / 4; e++) store_pack<TO, 4>(at + 8 * e, gv + 4 * e);
+      }
+      if (rb == RB - 1) {
+        const int64_t next = min(t + plan.row_groups, last), after = min(t + 2 * plan.row_groups, last);
+        put(buffer ^ 1);
+        fetch(after);
+        // a last tile that is not full is asked for once more behind the loop, row by row; here this one stands in for it
+        fetch_more(!PLAIN || (next + 1) * MR <= a.rows ? next : t, plain);
+      }
+      wave_order();
+      char *base = reinterpret_cast<char *>(static_cast<TO *>(a.out) + my_row * a.ld_out + n0);
+      const char *mine = s_own + orow * PO + l % OP * 16;
+      const int64_t left = a.rows - my_row;
+#pragma unroll
+      for (int j = 0; j < (GRAD ? 2 : 1) * NO; j++) {
+        TO *to = reinterpret_cast<TO *>(base + ((int64_t)(j % NO) * OROWS * a.ld_out + j / NO * a.pad) * (int)sizeof(TO) + o_at);
+        const Piece v = *reinterpret_cast<const Piece *>(mine + j * OROWS * PO);
+        if constexpr (PLAIN) *reinterpret_cast<PieceAny *>(to) = v;
+        else {
+          if (orow + j % NO * OROWS >= left) continue;
+          if (GRAD || n0 + ocol + OE <= a.hidden) *reinterpret_cast<PieceAny *>(to) = v;
+          else
+            for (int e = 0; n0 + ocol + e < a.hidden; e++) to[e] = reinterpret_cast<const TO *>(mine + j * OROWS * PO)[e];
+        }
+      }
+      wave_order();
+    }
+  };
+  put(0);
+  fetch(min(t + plan.row_groups, last));
+  int buffer = 0;
+  if (n0 >= (GRAD ? a.pad : a.hidden)) {     // a wave without columns loads rows with the others
+    for (; t <= last; t += plan.row_groups, buffer ^= 1) {
+      __syncthreads();
+      put(buffer ^ 1);
+      fetch(min(t + 2 * plan.row_groups, last));
+    }
+    return;
+  }
+  fetch_more(t, std::false_type());
+  if (GRAD || whole)
+    for (; t < last; t += plan.row_groups, buffer ^= 1) tile(t, buffer, std::true_type());
+  else
+    for (; t < last; t += plan.row_groups, buffer ^= 1) tile(t, buffer, std::false_type());
+  fetch_more(t, std::false_type());
+  tile(t, buffer, std::false_type());
 }
 
 // ------------------------------------------------------------------------------------ gradient
@@ -536,6 +798,54 @@ __global__ __launch_bounds__(kHeadThreads) void k_gated_few(GatedArgs a) {
 // ------------------------------------------------------------------------------------ host side
 constexpr int64_t kFewRows = 16, kFewResults = 64 * 1024;    // as ink_linear: each workgroup asks for its columns of both matrices again for every row
 
+// Many rows, and a depth whose weights fit the registers: workgroups for the whole card, each with a stream of row tiles.
+constexpr int64_t kStreamRows = 32 * 1024;
+template <class T, class TO, int KS, int WN, int WM, int PER, bool GRAD> static void stream_launch(const GatedArgs &a, Launches &run) {
+  constexpr int RB = stream_blocks<T, KS, WM>(), MR = 32 * RB * WM, P = KS * kTypeStep<T> * (int)sizeof(T) + 16, OWN = 32 * (32 * (int)sizeof(TO) + 16) * (GRAD ? 2 : 1), WAVES = WN * WM;
+  constexpr int lds = 2 * MR * P + WAVES * (OWN + (sizeof(T) == 1 ? 256 : 0)), per_cu = std::max(1, std::min((160 << 10) / lds, 4 * PER / WAVES));
+  static_assert(lds <= 160 << 10, "LDS holds two tiles of rows and the waves' results");
+  const int wide = GRAD ? a.pad : a.hidden;
+  StreamPlan p;
+  p.groups = (wide + 32 * WN - 1) / (32 * WN);
+  const int64_t tiles = (a.rows + MR - 1) / MR;
+  p.row_groups = (int)std::min<int64_t>((tiles + 7) / 8 * 8, std::max(8, 256 * per_cu / p.groups / 8 * 8));
+  run.lds = lds;
+  run(k_gated_stream<T, TO, KS, WN, WM, PER, GRAD>, dim3((unsigned)(p.groups * p.row_groups)), dim3(kWave * WAVES), a, p);
+  run.lds = 0;
+}
+// Four waves a workgroup, one on every SIMD of its CU (workgroups of six leave no room for a second one although its registers are there), or, where the
+// columns fill them about as well, twelve, three on every SIMD: rows of results then leave a workgroup whole, which counts where they are no multiple of
+// whole lines (2.45M x 128 x 341 bf16 722 us with twelve waves, 872 with three workgroups of four; x 344 660 and 765; x 384 654 and 692).
+template <class T, class TO, int KS, int PER, bool GRAD> static void stream_waves(const GatedArgs &a, Launches &run) {
+  const int tiles = ((GRAD ? a.pad : a.hidden) + 31) / 32;
+  if (tiles == 1) return stream_launch<T, TO, KS, 1, sizeof(T) == 4 ? 2 : 4, PER, GRAD>(a, run);
+  if (tiles == 2 || tiles == 5 || tiles == 6) return stream_launch<T, TO, KS, 2, 2, PER, GRAD>(a, run);
+  if constexpr (PER == 3)
+    if (tiles > 8 && (tiles + 11) / 12 * 12 <= (tiles + 3) / 4 * 4 + 1) return stream_launch<T, TO, KS, 12, 1, PER, GRAD>(a, run);
+  stream_launch<T, TO, KS, 4, 1, PER, GRAD>(a, run);
+}
+template <class T, class TO, bool GRAD> static bool stream_run(const GatedArgs &a, Launches &run) {
+  if (a.rows < kStreamRows || a.cols < 16 / (int)sizeof(T) || a.hidden < 16 / (int)sizeof(TO) || (sizeof(T) > 1 && a.hidden < 16 / (int)sizeof(T))) return false;
+  for (const int64_t ld : {a.ld_x, a.ld_out, a.ld_dh})
+    if (ld >= 1 << 22) return false;         // offsets within a tile are 32-bit
+  const int steps = (a.cols + kTypeStep<T> - 1) / kTypeStep<T>;
+  if constexpr (sizeof(T) == 4) {
+    if (steps <= 8) stream_waves<T, TO, 8, 3, GRAD>(a, run);
+    else if (steps <= 16) stream_waves<T, TO, 16, 2, GRAD>(a, run);
+    else return false;
+  } else if constexpr (sizeof(T) == 2) {
+    if (steps <= 8) stream_waves<T, TO, 8, 3, GRAD>(a, run);
+    else if (steps <= 16) stream_waves<T, TO, 16, 2, GRAD>(a, run);
+    else return false;
+  } else {
+    if (steps <= 2) stream_waves<T, TO, 2, 3, GRAD>(a, run);
+    else if (steps <= 4) stream_waves<T, TO, 4, 2, GRAD>(a, run);
+    else if (steps <= 8) stream_waves<T, TO, 8, 2, GRAD>(a, run);
+    else return false;
+  }
+  return true;
+}
+
 constexpr int64_t kLaunchRows = 1 << 21;     // a launch has fewer than 2^32 threads: so many rows by INK_MAX_IN_DIM columns are 2^30
 template <class TL, class T, class TO> static void gated_tiles(const GatedArgs &a, Launches &run) {
   const int gy = (a.hidden + kTileHidden - 1) / kTileHidden;
@@ -553,6 +863,8 @@ template <class T, class TO> static void gated_run(const GatedArgs &a, Launches 
   if constexpr (sizeof(T) != 1)
     if (a.rows <= kFewRows && a.rows * a.hidden <= kFewResults)
       return run(k_gated_few<T>, dim3((a.hidden + 31) / 32, (unsigned)a.rows), dim3(kHeadThreads), a);
+  if constexpr (sizeof(T) != 1 || sizeof(TO) != 4)
+    if (stream_run<T, TO, false>(a, run)) return;
   gated_tiles<T, std::conditional_t<sizeof(T) == 1 && sizeof(TO) == 4, bf16, T>, TO>(a, run);
 }
 
@@ -584,7 +896,7 @@ template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void 
     b.x = static_cast<const T *>(a.x) + r0 * a.ld_x;
     b.dh = static_cast<const T *>(a.dh) + r0 * a.ld_dh;
     const int64_t tiles = (b.rows + 127) / 128;
-    run(k_gated_tile<T, T, T, 2, true>, dim3((unsigned)((tiles + 7) / 8 * 8 * (p.pad / kTileHidden))), dim3(256), b);
+    if (!stream_run<T, T, true>(b, run)) run(k_gated_tile<T, T, T, 2, true>, dim3((unsigned)((tiles + 7) / 8 * 8 * (p.pad / kTileHidden))), dim3(256), b);
     if (dx) {
       GatedDxArgs q{work, a.gate, a.up, static_cast<T *>(dx) + r0 * ld_dx, b.rows, a.ld_gate, a.ld_up, ld_dx, a.cols, a.hidden, p.pad};
       run(k_gated_dx<T>, dim3((unsigned)((tiles + 7) / 8 * 8 * p.tiles_c)), dim3(256), q);

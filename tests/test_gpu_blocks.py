@@ -286,6 +286,52 @@ def test_gated_backward(rows, cols, hidden, dtype):
     assert head.gated_backward(*args, act=act, need_dx=False, need_dweights=False) == (None, None, None)
 
 
+# enough rows for the kernels that keep the weights in registers, or for their fallback (deep sums, few columns): every class of depth and
+# width, sizes beside the tiles', last tiles of one row, rows that no workgroup shares with another
+MANY = [(32768, 64, 32, 0), (32769, 128, 344, 3), (33000, 47, 31, 1), (32800, 100, 64, 2), (32769, 65, 172, 3), (32801, 8, 341, 0), (32790, 120, 130, 1),
+        (32777, 256, 100, 3), (33333, 250, 41, 2), (32769, 200, 300, 3), (32801, 7, 40, 1), (32769, 270, 50, 3), (32770, 33, 7, 2), (36000, 129, 8, 3)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,hidden,act", MANY)
+def test_gated_of_many_rows(rows, cols, hidden, act, dtype):
+    g = gen(rows + cols * 3 + hidden)
+    x, dh = torch.randn(rows, cols, generator=g).to(dtype), torch.randn(rows, hidden, generator=g).to(dtype)
+    wg, wu = ((torch.randn(cols, hidden, generator=g) * cols ** -0.5).to(dtype) for _ in range(2))
+    off = hidden % 4
+    args = (table(x, cols + off, off), table(wg, hidden + 2 * off, off), table(wu, hidden + off, off))
+    h = head.gated(*args, act=ACTS[act])
+    want, e = gated_ref(x.double(), wg.double(), wu.double(), ACTS[act], cols)
+    close(h, want, e, dtype, "h")
+    got = head.gated_backward(table(dh, hidden + off, off), *args, act=ACTS[act])
+    for a, (want, e), name in zip(got, gated_grad_ref(dh, x, wg, wu, ACTS[act], dtype), ("dx", "dw_gate", "dw_up")):
+        close(a, want, e, dtype, name)
+    view = torch.full((rows, hidden + 9), 7.0, dtype=dtype, device="cuda")   # results as columns of a wider table: nothing beside them is written
+    lib, stream, t = head._functions(), torch.cuda.current_stream().cuda_stream, head.TYPES[dtype]
+    xd, gd, ud = x.cuda(), wg.cuda(), wu.cuda()
+    assert lib.ink_gated(xd.data_ptr(), cols, None, gd.data_ptr(), hidden, ud.data_ptr(), hidden, None, None, rows, cols, hidden, t, t, act,
+                         view[:, 4:].data_ptr(), hidden + 9, stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(view[:, 4:4 + hidden], h), "the layout of the tensors changed the result"
+    assert (view[:, :4] == 7).all() and (view[:, 4 + hidden:] == 7).all()
+
+
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("rows,cols,hidden,act", [(32769, 256, 130, 2), (33000, 128, 344, 3), (32801, 100, 31, 1), (32770, 16, 64, 0), (32769, 500, 70, 3), (32800, 520, 33, 1),
+                                                  (32768, 15, 40, 3), (32769, 193, 5, 2)])
+def test_gated_of_many_8_bit_rows(rows, cols, hidden, act, out):
+    g = gen(rows + cols * 3 + hidden)
+    x, xs = to_codes(torch.randn(rows, cols, generator=g), 1)
+    wg, sg = to_codes(torch.randn(hidden, cols, generator=g) * cols ** -0.5, 1)
+    wu, su = to_codes(torch.randn(hidden, cols, generator=g) * cols ** -0.5, 1)
+    dx, dg, du = x.double() * xs.double()[:, None], (wg.double() * sg.double()[:, None]).t(), (wu.double() * su.double()[:, None]).t()
+    h = head.gated(x.cuda(), wg.cuda().t(), wu.cuda().t(), act=ACTS[act], out_dtype=out, x_scale=xs.cuda(), gate_scale=sg.cuda(), up_scale=su.cuda())
+    # of every product of a row and a column at most its largest factors'
+    more = None if out is F32 else tuple(cols * 2.0 ** -14 * dx.abs().amax(1)[:, None] * w.abs().amax(0) for w in (dg, du))
+    want, e = gated_ref(dx, dg, du, ACTS[act], cols, more)
+    close(h, want, e, out, "h")
+
+
 def test_gated_gradient_against_differences():
     g = gen(4)
     x, dh = torch.randn(5, 7, generator=g), torch.randn(5, 6, generator=g)
