@@ -62,11 +62,12 @@ __device__ __forceinline__ uint32_t code_by_chance(float a, uint32_t random) {
 // Eight numbers of a block to codes and the block's scale, which all sixteen lanes of the block get.  With a number that is
 // none the scale is none.
 template <bool ROOT> __device__ __forceinline__ float to_codes(const float x[8], const uint32_t random[8], uint32_t code[2]) {
+#pragma clang fp contract(off)
   float top = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; j++) top = fmaxf(top, fabsf(x[j]) <= 3.4028235e38f ? fabsf(x[j]) : INFINITY);
   top = group_all<16>(top, [](float a, float b) { return fmaxf(a, b); });
-  const float scale = top == INFINITY ? NAN : top < 448.f * 1.17549435e-38f ? 0.f : top / 448.f;
+  const float scale = top == INFINITY ? NAN : top < 448.f * 1.17549435e-38f ? 0.f : top * (1.f / 448.f);
   const float by = scale > 0.f ? 1.f / scale : 0.f;
   code[0] = code[1] = 0;
 #pragma unroll
@@ -119,6 +120,9 @@ struct None {};                            // no copy
 
 template <class TP, class TG, class TC, bool EIGHT>
 __global__ __launch_bounds__(kHeadThreads) void k_adamw(AdamArgs a) {
+  // Every operation is rounded by itself, none fused: a plain program of the same formulas then has the same bits, and the same codes (a number
+  // that differs in its last bit falls on the other side of a random number now and then).  Memory bounds the kernel either way.
+#pragma clang fp contract(off)
   constexpr bool CHANCE = EIGHT || sizeof(TP) == 2;
   int k = 0;
 #pragma unroll

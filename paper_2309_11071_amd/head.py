@@ -10,6 +10,7 @@ Tensors of other devices or types and shapes that do not fit raise.
 """
 import array
 import ctypes as C
+import itertools
 
 import torch
 
@@ -411,18 +412,25 @@ def adamw_moments(params, bits=32):
     return made
 
 
-def _held(t, name, like, dtypes):
-    """The address of a tensor that a step changes in place: of the parameter's shape and device, contiguous."""
-    if not isinstance(t, torch.Tensor) or t.shape != like.shape or t.device != like.device:
-        raise ValueError("%s must be a tensor of its parameter's shape, on its device" % name)
-    if t.dtype not in dtypes:
-        raise TypeError("%s has type %s, wanted %s" % (name, t.dtype, " or ".join(str(d) for d in dtypes)))
-    if not t.is_contiguous():
+_numel, _address, _contiguous, _device_index = torch.Tensor.numel, torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
+
+
+def _held(ts, name, sizes, dev, dtypes):
+    """Addresses of the tensors that a step changes in place: contiguous, of these numbers of elements, on the GPU `dev`.  All of a list at
+    a time: a head has hundreds of tensors, and a call should take less than the step."""
+    types = {t.dtype for t in ts}
+    if not types <= dtypes:
+        raise TypeError("%s has type %s, wanted %s" % (name, (types - dtypes).pop(), " or ".join(sorted(map(str, dtypes)))))
+    if set(map(_device_index, ts)) != {dev}:
+        raise ValueError("%s is not on the parameters' GPU" % name)
+    if list(map(_numel, ts)) != sizes:
+        raise ValueError("%s has another number of elements than its parameter calls for" % name)
+    if not all(map(_contiguous, ts)):
         raise ValueError("%s must be contiguous: the step changes it in place" % name)
-    return t.data_ptr()
+    return list(map(_address, ts))
 
 
-_PARAMS, _COPIES, _CODES, _ANY = (torch.float32, torch.bfloat16), (torch.bfloat16, torch.float16), (E4M3,), tuple(TYPES)
+_PARAMS, _COPIES, _CODES, _SCALES = {torch.float32, torch.bfloat16}, {torch.bfloat16, torch.float16}, {E4M3}, {torch.float32}
 
 
 def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=1.0, copies=None, seed=0):
@@ -436,69 +444,69 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
     n = len(params)
     if len(grads) != n or len(moments) != n or (copies is not None and len(copies) != n):
         raise ValueError("params, grads, moments and copies must have one entry for each parameter")
-    given = [i for i in range(n) if grads[i] is not None]
-    if not given:
+    place = [i for i in range(n) if grads[i] is not None]
+    if not place:
         return
-    like = params[given[0]]
-    if not isinstance(like, torch.Tensor) or not like.is_cuda:
+    some = len(place) < n
+    p, g, mom = ([x[i] for i in place] for x in (params, grads, moments)) if some else (list(params), list(grads), moments)
+    like, n = p[0], len(p)
+    dev = like.get_device()
+    if dev < 0:
         raise ValueError("params must be GPU tensors")
-    width = len(moments[given[0]])
-    if width not in (2, 4):
-        raise ValueError("moments must be adamw_moments': (m, v) or (m, m_scale, v, v_scale)")
-    groups, changed, kept, dev = {}, [], [], like.device
-    for i in given:
-        p, g, mom, copy = params[i], grads[i], moments[i], None if copies is None else copies[i]
-        at = _held(p, "a parameter", p, _PARAMS)
-        if p.device != dev:
-            raise ValueError("the parameters are on several devices")
-        if p.requires_grad and not p.is_leaf:
-            _unrecorded(p, "a parameter that is no leaf")
-        if g.shape != p.shape or g.device != dev or g.dtype not in TYPES:
-            raise ValueError("a gradient has shape %s and type %s on %s, its parameter shape %s on %s" % (tuple(g.shape), g.dtype, g.device, tuple(p.shape), dev))
-        if g.requires_grad:
-            _unrecorded(g, "a gradient")
-        if not g.is_contiguous():
-            g = g.contiguous()
-            kept.append(g)
-        size, c = p.numel(), 0
-        if len(mom) != width:
-            raise ValueError("moments of 32 and of 8 bits in one call")
-        if width == 2:
-            held = [at, _held(mom[0], "a first moment", p, _F32), _held(mom[1], "a second moment", p, _F32)]
-            m, v, ms, vs = held[1], held[2], 0, 0
-        else:
-            m, v, blocks = _held(mom[0], "a first moment", p, _CODES), _held(mom[2], "a second moment", p, _CODES), -(-size // ADAMW_BLOCK)
-            for s in (mom[1], mom[3]):
-                if s.dtype is not torch.float32 or s.device != dev or s.shape != (blocks,) or not s.is_contiguous():
-                    raise ValueError("a moment's scales must be a contiguous float32 tensor of shape [%d] on the parameter's device" % blocks)
-            ms, vs = mom[1].data_ptr(), mom[3].data_ptr()
-            held = [at, m, v, ms, vs]
-        if copy is not None:
-            if p.dtype is not torch.float32:
-                raise TypeError("a copy is of float32 parameters")
-            c = _held(copy, "a copy", p, _COPIES)
-            held.append(c)
-        if size:
-            changed += held
-        groups.setdefault((p.dtype, g.dtype, None if copy is None else copy.dtype), []).append((at, g.data_ptr(), c, m, v, ms, vs, size, i))
+    width = len(mom[0])
+    if width not in (2, 4) or any(len(m) != width for m in mom):
+        raise ValueError("moments must be adamw_moments', all of one width")
+    sizes = list(map(_numel, p))
+    at = _held(p, "a parameter", sizes, dev, _PARAMS)
+    if any(x.requires_grad and not x.is_leaf for x in p) and torch.is_grad_enabled():
+        raise ValueError("a parameter that requires a gradient and is no leaf cannot be changed in place")
+    if not {x.dtype for x in g} <= TYPES.keys() or set(map(_device_index, g)) != {dev} or any(x.shape != y.shape for x, y in zip(g, p)):
+        raise ValueError("a gradient must be a float32, bfloat16 or float16 tensor of its parameter's shape, on its GPU")
+    if any(x.requires_grad for x in g):
+        _unrecorded(g, "a gradient")
+    if not all(map(_contiguous, g)):
+        g = [x.contiguous() for x in g]
+    if width == 2:
+        held = [_held([m[0] for m in mom], "a first moment", sizes, dev, _SCALES), None, _held([m[1] for m in mom], "a second moment", sizes, dev, _SCALES), None]
+    else:
+        blocks = [-(-s // ADAMW_BLOCK) for s in sizes]
+        held = [_held([m[0] for m in mom], "a first moment", sizes, dev, _CODES), _held([m[1] for m in mom], "a scale of first moments", blocks, dev, _SCALES),
+                _held([m[2] for m in mom], "a second moment", sizes, dev, _CODES), _held([m[3] for m in mom], "a scale of second moments", blocks, dev, _SCALES)]
+    none = [0] * n
+    c, here, copy = none, [], [None] * n
+    if copies is not None:
+        copy = [copies[i] for i in place] if some else copies
+        here = [i for i in range(n) if copy[i] is not None]
+        if any(p[i].dtype is not torch.float32 for i in here):
+            raise TypeError("a copy is of float32 parameters")
+        if here:
+            c = list(none)
+            for i, x in zip(here, _held([copy[i] for i in here], "a copy", [sizes[i] for i in here], dev, _COPIES)):
+                c[i] = x
+    # (tensors without elements have no address of their own)
+    changed = [x for column in (at, *held, c) if column is not None and column is not none for x, s in zip(column, sizes) if s and x]
     if len(set(changed)) != len(changed):
         raise ValueError("a tensor that the step changes stands in the call twice")
     step_at = scale_at = None
     if isinstance(step, torch.Tensor):
-        if step.dtype is not torch.int64 or step.numel() != 1 or step.device != dev:
+        if step.dtype is not torch.int64 or step.numel() != 1 or step.get_device() != dev:
             raise ValueError("step must be a number or an int64 tensor of one element on the parameters' device")
         step_at, step = step.data_ptr(), 1
     if isinstance(grad_scale, torch.Tensor):
-        if grad_scale.dtype is not torch.float32 or grad_scale.numel() != 1 or grad_scale.device != dev:
+        if grad_scale.dtype is not torch.float32 or grad_scale.numel() != 1 or grad_scale.get_device() != dev:
             raise ValueError("grad_scale must be a number or a float32 tensor of one element on the parameters' device")
         if grad_scale.requires_grad:
             _unrecorded(grad_scale, "grad_scale")
         scale_at, grad_scale = grad_scale.data_ptr(), 1.0
     lib = _functions()
-    for (tp, tg, tc), entries in groups.items():
-        table = array.array("q", [x for e in entries for x in e])
-        _call(lib.ink_adamw, like, table.buffer_info()[0], len(entries), TYPES[tp], TYPES[tg], -1 if tc is None else TYPES[tc], 8 if width == 4 else 32, lr,
+    entries = list(zip(at, map(_address, g), c, held[0], held[2], held[1] or none, held[3] or none, sizes, place))
+    kinds = [(x.dtype, y.dtype, None if z is None else z.dtype) for x, y, z in zip(p, g, copy)]
+    for kind in dict.fromkeys(kinds):
+        table = array.array("q", itertools.chain.from_iterable(e for e, k in zip(entries, kinds) if k == kind))
+        tp, tg, tc = kind
+        _call(lib.ink_adamw, like, table.buffer_info()[0], len(table) // 9, TYPES[tp], TYPES[tg], -1 if tc is None else TYPES[tc], 8 if width == 4 else 32, lr,
               betas[0], betas[1], eps, weight_decay, step, step_at, grad_scale, scale_at, seed & 0xFFFFFFFFFFFFFFFF)
     # what autograd has kept of these tensors is no longer what they hold
-    torch.autograd.graph.increment_version([t for i in given for t in (params[i], None if copies is None else copies[i])
-                                            if t is not None])
+    torch.autograd.graph.increment_version(p)
+    if here:
+        torch.autograd.graph.increment_version([copy[i] for i in here])

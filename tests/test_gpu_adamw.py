@@ -290,3 +290,75 @@ def test_more_than_2_32_elements():
     assert abs(float(mom[0][1][-1]) * 448 - (1 - B1) * g0) <= 4 * u * g0
     del p, g, mom
     torch.cuda.empty_cache()
+
+
+def test_refusals():
+    p = [torch.zeros(300, device="cuda") for _ in range(2)]
+    g = [torch.ones(300, device="cuda") for _ in range(2)]
+    mom, mom8 = head.adamw_moments(p), head.adamw_moments(p, 8)
+    bf = [x.to(BF16) for x in p]
+
+    def refused(kind, *args, **k):
+        with pytest.raises(kind):
+            head.adamw(*args, **k)
+    refused(ValueError, [p[0], p[0]], g, mom, 1)                              # one tensor twice
+    refused(ValueError, p, g, [mom[0], mom[0]], 1)
+    refused(ValueError, p, g, mom, 1, copies=[bf[0], bf[0]])
+    refused(ValueError, [p[0], p[0][:0]], g, mom, 1)
+    refused(ValueError, p, [g[0], g[1][:299]], mom, 1)
+    refused(ValueError, p, [g[0], g[1].view(3, 100)], mom, 1)
+    refused(ValueError, p, [g[0], g[1].cpu()], mom, 1)
+    refused(ValueError, p, [g[0], g[1].double()], mom, 1)
+    refused(ValueError, p, g, [mom[0], mom8[1]], 1)
+    refused(ValueError, p, g, [mom[0]], 1)
+    refused(TypeError, [x.half() for x in p], g, mom, 1)
+    refused(TypeError, p, g, [(m.half(), v) for m, v in mom], 1)
+    refused(TypeError, bf, g, mom, 1, copies=[x.clone() for x in bf])
+    refused(TypeError, p, g, mom, 1, copies=[x.clone() for x in p])
+    refused(ValueError, p, g, [(m, ms[:2], v, vs) for m, ms, v, vs in mom8], 1)
+    wide = torch.zeros(300, 2, device="cuda")
+    refused(ValueError, [wide[:, 0], p[1]], g, mom, 1)                        # not contiguous
+    refused(ValueError, p, g, mom, torch.tensor(1))                           # on the host
+    refused(ValueError, p, g, mom, torch.tensor([1, 2], device="cuda"))
+    refused(ValueError, p, g, mom, 1, grad_scale=torch.ones(1, device="cuda").double())
+    refused(ValueError, p, [x.requires_grad_() for x in g], mom, 1)
+    g = [x.detach() for x in g]
+    for k in (dict(lr=-1.0), dict(betas=(1.0, 0.9)), dict(eps=0.0), dict(weight_decay=float("nan")), dict(grad_scale=float("inf"))):
+        refused(head.InkError, p, g, mom, 1, **k)
+    refused(head.InkError, p, g, mom, 0)
+    assert not any(x.any() for x in p + [m for e in mom for m in e]), "nothing was changed"
+    q = torch.zeros(4, device="cuda", requires_grad=True)
+    refused(ValueError, [q * 1], [torch.ones(4, device="cuda")], head.adamw_moments([q]), 1)
+
+
+def test_autograd_sees_the_change():
+    """What autograd keeps of a parameter for a backward pass is out of date after the step; a leaf that requires a gradient is an ordinary parameter."""
+    q, x = torch.ones(4, device="cuda", requires_grad=True), torch.ones(4, device="cuda", requires_grad=True)
+    loss = (q * x).sum()
+    head.adamw([q], [torch.ones(4, device="cuda")], head.adamw_moments([q]), 1, lr=0.5, weight_decay=0.0)
+    assert torch.allclose(q.detach(), torch.full((4,), 0.5, device="cuda"))
+    with pytest.raises(RuntimeError):
+        loss.backward()
+    with torch.inference_mode():
+        r = torch.ones(4, device="cuda")
+        head.adamw([r], [r.clone()], head.adamw_moments([r]), 1, lr=0.5, weight_decay=0.0)
+        assert torch.allclose(r, torch.full((4,), 0.5, device="cuda"))
+
+
+def test_another_stream():
+    """The step runs on the current stream: behind what was enqueued there, whatever the default stream does."""
+    e = state(200_000, F32, F32, None, 8, torch.Generator().manual_seed(4))
+    twin = [x.clone() for x in (e[0], *e[2])]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        late = e[1].clone()
+        for _ in range(20):
+            late.mul_(1.25)
+        for _ in range(20):
+            late.mul_(0.8)
+        head.adamw([e[0]], [late], [e[2]], 3, seed=1)
+    side.synchronize()
+    head.adamw([twin[0]], [late], [tuple(twin[1:])], 3, seed=1)
+    for x, y in zip((e[0], *e[2]), twin):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
