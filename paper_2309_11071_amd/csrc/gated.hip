@@ -23,50 +23,46 @@ __device__ __forceinline__ f32x16 mma(Frag<e4m3>::V a, Frag<e4m3>::V b, f32x16 c
 typedef int Piece __attribute__((ext_vector_type(4)));                // 16 bytes
 typedef int PieceAny __attribute__((ext_vector_type(4), aligned(1)));
 
-// Elements k .. of a row of n elements, as many as a piece holds; past the row's end zeros, and nothing is read there.
-template <class T> __device__ __forceinline__ Piece row_piece(const T *row, int k, int n) {
-  constexpr int N = 16 / sizeof(T);
-  if (k + N <= n) return (Piece)*reinterpret_cast<const PieceAny *>(row + k);
-  Piece v{};
-  if constexpr (sizeof(T) == 1) {
-    uint32_t w[4] = {0, 0, 0, 0};
+// Elements k .. of a row of n elements of TL, as many as a piece of T holds (8-bit numbers may become 16-bit ones on the way); past the row's end
+// zeros, and nothing is read there.  In two steps, so that nothing waits for the load where it is asked for: a piece that the row's
+// end cuts is the row's last bytes, which piece_of moves down.  SHORT: rows that hold no whole piece, element by element.
+template <class TL, class T> struct RawOf { typedef Piece V; };
+template <> struct RawOf<e4m3, bf16> { typedef uint64_t V; };
+template <class TL, class T, bool SHORT> __device__ __forceinline__ typename RawOf<TL, T>::V raw_piece(const TL *row, int k, int n) {
+  typedef typename RawOf<TL, T>::V V;
+  constexpr int N = sizeof(V) / sizeof(TL);
+  if constexpr (SHORT) {
+    typedef std::conditional_t<sizeof(TL) == 1, uint8_t, std::conditional_t<sizeof(TL) == 2, uint16_t, uint32_t>> Bits;
+    unsigned __int128 v = 0;
 #pragma unroll
     for (int j = 0; j < N; j++)
-      if (k + j < n) w[j / 4] |= (uint32_t)row[k + j] << 8 * (j % 4);
-#pragma unroll
-    for (int j = 0; j < 4; j++) v[j] = (int)w[j];
-  } else {
-    typedef T R __attribute__((ext_vector_type(N)));
-    R r{};
-#pragma unroll
-    for (int j = 0; j < N; j++) r[j] = k + j < n ? row[k + j] : (T)0.f;
-    v = __builtin_bit_cast(Piece, r);
-  }
-  return v;
+      if (k + j < n) v |= (unsigned __int128)reinterpret_cast<const Bits *>(row)[k + j] << (8 * sizeof(TL) * j);
+    if constexpr (sizeof(V) == 8) return (uint64_t)v;
+    else return __builtin_bit_cast(Piece, v);
+  } else if constexpr (sizeof(V) == 8) {
+    typedef uint64_t W __attribute__((aligned(1)));
+    return *reinterpret_cast<const W *>(row + min(k, n - N));
+  } else return (Piece)*reinterpret_cast<const PieceAny *>(row + min(k, n - N));
 }
-
-// Elements k .. of a row of TL as a piece of T: 8-bit numbers may become 16-bit ones on the way.
-template <class TL, class T> __device__ __forceinline__ Piece row_piece_as(const TL *row, int k, int n) {
-  if constexpr (sizeof(TL) == sizeof(T)) return row_piece(row, k, n);
-  else {
-    uint32_t w[2] = {0, 0};
-    if (k + 8 <= n) {
-      typedef uint32_t W __attribute__((ext_vector_type(2), aligned(1)));
-      const W v = *reinterpret_cast<const W *>(row + k);
-      w[0] = v[0]; w[1] = v[1];
-    } else
-#pragma unroll
-      for (int j = 0; j < 8; j++)
-        if (k + j < n) w[j / 4] |= (uint32_t)row[k + j] << 8 * (j % 4);
+template <class TL, class T, bool SHORT> __device__ __forceinline__ Piece piece_of(typename RawOf<TL, T>::V v, int k, int n) {
+  typedef typename RawOf<TL, T>::V V;
+  constexpr int N = sizeof(V) / sizeof(TL);
+  if constexpr (!SHORT)
+    if (k + N > n) {
+      if constexpr (sizeof(V) == 8) v = k < n ? v >> 8 * (k + N - n) : 0;
+      else v = k < n ? move_down(v, k + N - n, sizeof(TL)) : Piece{};
+    }
+  if constexpr (sizeof(V) == 8) {
     typedef T R __attribute__((ext_vector_type(8)));
     R r;
 #pragma unroll
     for (int j = 0; j < 2; j++) {
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
+      const int w = (int)(uint32_t)(v >> 32 * j);
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
       r[4 * j] = (T)lo[0]; r[4 * j + 1] = (T)lo[1]; r[4 * j + 2] = (T)hi[0]; r[4 * j + 3] = (T)hi[1];
     }
     return __builtin_bit_cast(Piece, r);
-  }
+  } else return v;
 }
 
 struct GatedArgs {
@@ -74,7 +70,7 @@ struct GatedArgs {
   const float *x_scale, *gate_scale, *up_scale;
   void *out;                                 // forward: h; gradient: [rows][2 pad] of dg and du
   int64_t rows, ld_x, ld_gate, ld_up, ld_dh, ld_out;
-  int cols, hidden, act, pad;                // pad: hidden rounded up to whole tiles
+  int cols, hidden, act, pad;                // pad: hidden rounded up to 32
 };
 
 constexpr int kChunk = 128, kChunkPitch = kChunk + 16;     // bytes of the depth in LDS at a time, and between rows there
@@ -145,12 +141,12 @@ template <int N> __device__ __forceinline__ void gate_grad_all(float g[N], float
 // ------------------------------------------------------------------------------------ tiles
 // 64 RB rows by 64 columns of h a workgroup, 32 RB by 32 a wave (a tile of Wg and one of Wu, so that g and u of an element meet in a lane).
 // TL: type of the operands in memory, T: in the products, TO: of h.  GRAD: dg and du go to `out` in place of h.
-template <class TL, class T, class TO, int RB, bool GRAD>
+template <class TL, class T, class TO, int RB, bool GRAD, bool SHORT>
 __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
   typedef typename Frag<T>::V V;
   constexpr int BM = 64 * RB, KC = kChunkK<T>, PE = 16 / sizeof(T), STEPS = KC / kTypeStep<T>;
   constexpr bool DEEP = sizeof(TL) != 1;     // the depth runs down the weights' columns
-  constexpr int PW = DEEP ? 2 * kTileHidden * (int)sizeof(T) + 16 : kChunkPitch;
+  constexpr int PW = DEEP ? 2 * kTileHidden * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 16) : kChunkPitch;
   constexpr int NX = BM * 8 / 256, NW = 4;
   constexpr int PO = kTileHidden * (int)sizeof(TO) + 16;
   constexpr int kLoop = BM * kChunkPitch + (DEEP ? KC : 2 * kTileHidden) * PW, kEnd = BM * PO * (GRAD ? 2 : 1);
@@ -162,44 +158,46 @@ __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
   const int64_t m0 = ((int64_t)(id / gy) * 8 + blockIdx.x % 8) * BM;
   const int n0 = id % gy * kTileHidden;
   if (m0 >= a.rows) return;
-  Piece x[NX], w[NW];
+  typename RawOf<TL, T>::V x[NX], w[NW];
   const TL *xp[NX];
 #pragma unroll
   for (int j = 0; j < NX; j++) xp[j] = static_cast<const TL *>(a.x) + min(m0 + tid / 8 + 32 * j, a.rows - 1) * a.ld_x;
+  // This thread's pieces of the weights: a place in rows of Wg and Wu, some rows apart (rows of the weights, or of what is multiplied with one column).
+  constexpr int C = DEEP ? kTileHidden / PE : 8, WR = DEEP ? 256 / (2 * C) : 32;       // pieces of a row of Wg; rows apart
+  const int wc = DEEP ? tid % (2 * C) : tid % 8;
+  const bool up = DEEP && wc >= C;
+  const int wn_at = n0 + wc % C * PE;        // DEEP: first column
   auto fetch = [&](int k0) {
 #pragma unroll
-    for (int j = 0; j < NX; j++) x[j] = row_piece_as<TL, T>(xp[j], k0 + tid % 8 * PE, a.cols);
+    for (int j = 0; j < NX; j++) x[j] = raw_piece<TL, T, SHORT>(xp[j], k0 + tid % 8 * PE, a.cols);
 #pragma unroll
     for (int j = 0; j < NW; j++) {
-      const int i = tid + 256 * j;
-      w[j] = Piece{};
       if constexpr (DEEP) {
-        constexpr int C = kTileHidden / PE;    // pieces of a row of Wg
-        const int k = k0 + i / (2 * C), c = i % (2 * C), n = n0 + c % C * PE;
-        const TL *row = static_cast<const TL *>(c < C ? a.gate : a.up) + (int64_t)k * (c < C ? a.ld_gate : a.ld_up);
-        if (k < a.cols && n < a.hidden) w[j] = row_piece_as<TL, T>(row, n, a.hidden);
+        const int k = min(k0 + tid / (2 * C) + WR * j, a.cols - 1);
+        w[j] = raw_piece<TL, T, SHORT>(static_cast<const TL *>(up ? a.up : a.gate) + (int64_t)k * (up ? a.ld_up : a.ld_gate), wn_at, a.hidden);
       } else {
-        const int c = i / 8, n = n0 + c % kTileHidden;
-        const TL *row = static_cast<const TL *>(c < kTileHidden ? a.gate : a.up) + (int64_t)n * (c < kTileHidden ? a.ld_gate : a.ld_up);
-        if (n < a.hidden) w[j] = row_piece_as<TL, T>(row, k0 + i % 8 * PE, a.cols);
+        const int n = min(n0 + (tid / 8 + 32 * j) % kTileHidden, a.hidden - 1);
+        w[j] = raw_piece<TL, T, SHORT>(static_cast<const TL *>(j >= 2 ? a.up : a.gate) + (int64_t)n * (j >= 2 ? a.ld_up : a.ld_gate), k0 + wc * PE, a.cols);
       }
     }
   };
-  auto put = [&]() {
+  auto put = [&](int k0) {
 #pragma unroll
-    for (int j = 0; j < NX; j++) *reinterpret_cast<Piece *>(s_x + (tid / 8 + 32 * j) * kChunkPitch + tid % 8 * 16) = x[j];
+    for (int j = 0; j < NX; j++)
+      *reinterpret_cast<Piece *>(s_x + (tid / 8 + 32 * j) * kChunkPitch + tid % 8 * 16) = piece_of<TL, T, SHORT>(x[j], k0 + tid % 8 * PE, a.cols);
 #pragma unroll
     for (int j = 0; j < NW; j++) {
-      const int i = tid + 256 * j;
-      constexpr int C = DEEP ? 2 * kTileHidden / PE : 8;
-      *reinterpret_cast<Piece *>(s_w + i / C * PW + i % C * 16) = w[j];
+      if constexpr (DEEP) {                    // rows past the depth are zeros, as x is there
+        const int k = tid / (2 * C) + WR * j;
+        *reinterpret_cast<Piece *>(s_w + k * PW + wc * 16) = k0 + k < a.cols ? piece_of<TL, T, SHORT>(w[j], wn_at, a.hidden) : Piece{};
+      } else *reinterpret_cast<Piece *>(s_w + (tid / 8 + 32 * j) * PW + wc * 16) = piece_of<TL, T, SHORT>(w[j], k0 + wc * PE, a.cols);
     }
   };
   f32x16 g[RB], u[RB];
 #pragma unroll
   for (int i = 0; i < RB; i++) g[i] = u[i] = f32x16{};
   fetch(0);
-  put();
+  put(0);
   __syncthreads();
   for (int k0 = 0; k0 < a.cols; k0 += KC) {
     const bool more = k0 + KC < a.cols;
@@ -232,7 +230,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
         }
     }
     __syncthreads();
-    if (more) put();
+    if (more) put(k0 + KC);
     __syncthreads();
   }
   // Through LDS, so that dh is read and h, dg and du are written in whole lines.
@@ -242,9 +240,8 @@ __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
     for (int j = 0; j < NO; j++) {
       const int i = tid + 256 * j, row = i / OP, c = i % OP;
       const int64_t r = min(m0 + row, a.rows - 1);
-      Piece v{};
-      if (n0 + c * OE < a.hidden) v = row_piece(static_cast<const TO *>(a.dh) + r * a.ld_dh, n0 + c * OE, a.hidden);
-      *reinterpret_cast<Piece *>(s_mem + row * PO + c * 16) = v;
+      const Piece v = raw_piece<TO, TO, SHORT>(static_cast<const TO *>(a.dh) + r * a.ld_dh, n0 + c * OE, a.hidden);
+      *reinterpret_cast<Piece *>(s_mem + row * PO + c * 16) = piece_of<TO, TO, SHORT>(v, n0 + c * OE, a.hidden);
     }
     __syncthreads();
   }
@@ -286,7 +283,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
     for (int j = 0; j < 2 * NO; j++) {
       const int i = tid + 256 * j, row = i / OP, c = i % OP, part = row / BM;
       const int64_t r = m0 + row % BM;
-      if (r < a.rows)
+      if (r < a.rows && n0 + c * OE < a.pad)
         *reinterpret_cast<Piece *>(static_cast<TO *>(a.out) + r * a.ld_out + part * a.pad + n0 + c * OE) = *reinterpret_cast<const Piece *>(s_mem + row * PO + c * 16);
     }
   } else {
@@ -555,175 +552,225 @@ __global__ __launch_bounds__(kWave * WN * WM, PER) void k_gated_stream(GatedArgs
 }
 
 // ------------------------------------------------------------------------------------ gradient
-// dx = dg Wg^T + du Wu^T of the rows of one call of k_gated_tile: 128 rows by 128 columns a workgroup, 64 by 64 a wave.
+// dx = dg Wg^T + du Wu^T of the rows of one part: 128 rows by 128 columns a workgroup, 64 by 64 a wave.  (128 by 64 a wave reads a quarter less
+// of LDS, but leaves room for two workgroups a CU instead of three: 233k x 256 x 683 347 us instead of 366, 100k x 602 x 1605 633 instead of 588.)
 struct GatedDxArgs {
   const void *d, *gate, *up;                 // [rows][2 pad] of dg and du
   void *dx;
   int64_t rows, ld_gate, ld_up, ld_dx;
   int cols, hidden, pad;
 };
-template <class T>
+template <class T, bool SHORT>
 __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedDxArgs a) {
   typedef typename Frag<T>::V V;
-  constexpr int KC = kChunkK<T>, PE = 16 / sizeof(T), BM = 128, BN = 128, P = kChunkPitch;
-  constexpr int PO = BN * (int)sizeof(T) + 16, kLoop = (BM + BN) * P, kEnd = BM * PO;
+  constexpr int RI = 2, WM = 2, WN = 2, THREADS = 256, KC = kChunkK<T>, PE = 16 / sizeof(T), BM = 32 * RI * WM, BN = 64 * WN, P = kChunkPitch;
+  constexpr int ND = BM * 8 / THREADS, NW = BN * 8 / THREADS, RS = THREADS / 8;
+  constexpr int PO = BN * (int)sizeof(T) + 16, HALF = 16 * RI, kLoop = (BM + BN) * P, kEnd = HALF * WM * PO;      // results leave in two halves of a wave's rows
   __shared__ __align__(16) char s_mem[kLoop > kEnd ? kLoop : kEnd];
   char *s_d = s_mem, *s_w = s_mem + BM * P;
-  const int tid = threadIdx.x, l = lane_id(), half = l / 32, wm = tid / kWave / 2, wn = tid / kWave % 2;
+  const int tid = threadIdx.x, l = lane_id(), half = l / 32, wave = __builtin_amdgcn_readfirstlane(tid / kWave), wm = wave / WN, wn = wave % WN;
   const int gy = (a.cols + BN - 1) / BN, id = blockIdx.x / 8;
   const int64_t m0 = ((int64_t)(id / gy) * 8 + blockIdx.x % 8) * BM;
   const int n0 = id % gy * BN;
   if (m0 >= a.rows) return;
-  Piece d[4], w[4];
-  const T *dp[4];
+  Piece d[ND], w[NW];
+  const int at = tid % 8 * PE, row = tid / 8;
+  const T *dp = static_cast<const T *>(a.d) + m0 * 2 * a.pad + at;
+  uint32_t d_row[ND];
 #pragma unroll
-  for (int j = 0; j < 4; j++) dp[j] = static_cast<const T *>(a.d) + min(m0 + tid / 8 + 32 * j, a.rows - 1) * 2 * a.pad;
+  for (int j = 0; j < ND; j++) d_row[j] = (uint32_t)(min((int64_t)(row + RS * j), a.rows - 1 - m0) * 2 * a.pad);
   auto fetch = [&](int k0) {
-    const bool second = k0 >= a.pad;
-    const int k = k0 - (second ? a.pad : 0) + tid % 8 * PE;
+#pragma unroll
+    for (int j = 0; j < ND; j++) d[j] = *reinterpret_cast<const Piece *>(dp + d_row[j] + k0);
+    const bool second = k0 + at >= a.pad;
+    const int k = k0 + at - (second ? a.pad : 0);
     const T *from = static_cast<const T *>(second ? a.up : a.gate);
     const int64_t ld = second ? a.ld_up : a.ld_gate;
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      d[j] = *reinterpret_cast<const Piece *>(dp[j] + k0 + tid % 8 * PE);
-      const int n = n0 + tid / 8 + 32 * j;
-      w[j] = Piece{};
-      if (n < a.cols && k < a.hidden) w[j] = row_piece(from + (int64_t)n * ld, k, a.hidden);
-    }
+    for (int j = 0; j < NW; j++) w[j] = raw_piece<T, T, SHORT>(from + (int64_t)min(n0 + row + RS * j, a.cols - 1) * ld, k, a.hidden);
   };
-  auto put = [&]() {
+  auto put = [&](int k0) {
+    const int k = k0 + at - (k0 + at >= a.pad ? a.pad : 0);
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      *reinterpret_cast<Piece *>(s_d + (tid / 8 + 32 * j) * P + tid % 8 * 16) = d[j];
-      *reinterpret_cast<Piece *>(s_w + (tid / 8 + 32 * j) * P + tid % 8 * 16) = w[j];
-    }
+    for (int j = 0; j < ND; j++) *reinterpret_cast<Piece *>(s_d + (row + RS * j) * P + tid % 8 * 16) = d[j];
+#pragma unroll
+    for (int j = 0; j < NW; j++) *reinterpret_cast<Piece *>(s_w + (row + RS * j) * P + tid % 8 * 16) = piece_of<T, T, SHORT>(w[j], k, a.hidden);
   };
-  f32x16 acc[2][2];
+  f32x16 acc[RI][2];
 #pragma unroll
-  for (int i = 0; i < 2; i++) acc[i][0] = acc[i][1] = f32x16{};
+  for (int i = 0; i < RI; i++) acc[i][0] = acc[i][1] = f32x16{};
   fetch(0);
-  put();
+  put(0);
   __syncthreads();
   for (int k0 = 0; k0 < 2 * a.pad; k0 += KC) {
     const bool more = k0 + KC < 2 * a.pad;
     if (more) fetch(k0 + KC);
 #pragma unroll
     for (int s = 0; s < 4; s++) {
-      V ds[2], ws[2];
+      V ds[RI], ws[2];
 #pragma unroll
-      for (int i = 0; i < 2; i++) {
-        ds[i] = rows_frag<T>(s_d + (wm * 2 + i) * 32 * P, P, s);
-        ws[i] = rows_frag<T>(s_w + (wn * 2 + i) * 32 * P, P, s);
-      }
+      for (int n = 0; n < 2; n++) ws[n] = rows_frag<T>(s_w + (wn * 2 + n) * 32 * P, P, s);
+#pragma unroll
+      for (int i = 0; i < RI; i++) ds[i] = rows_frag<T>(s_d + (wm * RI + i) * 32 * P, P, s);
       mma_block<T>(ws, ds, acc);
     }
     __syncthreads();
-    if (more) put();
+    if (more) put(k0 + KC);
     __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < 2; i++)
-#pragma unroll
-    for (int n = 0; n < 2; n++)
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        const float v[4] = {acc[i][n][4 * e], acc[i][n][4 * e + 1], acc[i][n][4 * e + 2], acc[i][n][4 * e + 3]};
-        store_pack<T, 4>(reinterpret_cast<T *>(s_mem + ((wm * 2 + i) * 32 + l % 32) * PO) + (wn * 2 + n) * 32 + 8 * e + 4 * half, v);
-      }
-  __syncthreads();
   constexpr int OP = BN / PE;
 #pragma unroll
-  for (int j = 0; j < BM * OP / 256; j++) {
-    const int i = tid + 256 * j, row = i / OP, c = i % OP, n = n0 + c * PE;
-    const int64_t r = m0 + row;
-    if (r >= a.rows || n >= a.cols) continue;
-    T *to = static_cast<T *>(a.dx) + r * a.ld_dx + n;
-    if (n + PE <= a.cols) *reinterpret_cast<PieceAny *>(to) = *reinterpret_cast<const Piece *>(s_mem + row * PO + c * 16);
-    else {
-      const T *from = reinterpret_cast<const T *>(s_mem + row * PO) + c * PE;
-      for (int e = 0; n + e < a.cols; e++) to[e] = from[e];
+  for (int h = 0; h < 2; h++) {
+#pragma unroll
+    for (int i = 0; i < RI / 2; i++)
+#pragma unroll
+      for (int n = 0; n < 2; n++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float v[4] = {acc[RI / 2 * h + i][n][4 * e], acc[RI / 2 * h + i][n][4 * e + 1], acc[RI / 2 * h + i][n][4 * e + 2], acc[RI / 2 * h + i][n][4 * e + 3]};
+          store_pack<T, 4>(reinterpret_cast<T *>(s_mem + (wm * HALF + i * 32 + l % 32) * PO) + (wn * 2 + n) * 32 + 8 * e + 4 * half, v);
+        }
+    __syncthreads();
+    for (int i = tid; i < WM * HALF * OP; i += THREADS) {
+      const int r_in = i / OP, c = i % OP, n = n0 + c * PE;
+      const int64_t r = m0 + r_in / HALF * (32 * RI) + h * HALF + r_in % HALF;
+      if (r >= a.rows || n >= a.cols) continue;
+      T *to = static_cast<T *>(a.dx) + r * a.ld_dx + n;
+      if (n + PE <= a.cols) *reinterpret_cast<PieceAny *>(to) = *reinterpret_cast<const Piece *>(s_mem + r_in * PO + c * 16);
+      else {
+        const T *from = reinterpret_cast<const T *>(s_mem + r_in * PO) + c * PE;
+        for (int e = 0; n + e < a.cols; e++) to[e] = from[e];
+      }
     }
+    __syncthreads();
   }
 }
 
-// Sums over the rows of one call of k_gated_tile, x^T [dg du]: 128 columns of x by 128 of dg and du a workgroup, over a slice of the rows.  The sums of
-// the slice go to, or are added to, its partial matrix, in the fragments' order.
+// The same where tiles of 128 by 128 would leave most of the card without work: 32 rows by 32 columns a workgroup, whose eight waves share the depth and
+// take their fragments straight from memory (200 x 256 x 683 bf16: 20 us in tiles).
+template <class T, bool SHORT>
+__global__ __launch_bounds__(512) void k_gated_dx_small(GatedDxArgs a) {
+  typedef typename Frag<T>::V V;
+  constexpr int VK = kVec<T>, KS = kStep<T>, WAVES = 8;
+  __shared__ float s_acc[WAVES][32][36];
+  const int wave = threadIdx.x / kWave, l = lane_id(), half = l / 32;
+  const int64_t r0 = (int64_t)blockIdx.x * 32, r = min(r0 + l % 32, a.rows - 1);
+  const int n0 = blockIdx.y * 32, n = min(n0 + l % 32, a.cols - 1);
+  const T *d = static_cast<const T *>(a.d) + r * 2 * a.pad, *gate = static_cast<const T *>(a.gate) + n * a.ld_gate, *up = static_cast<const T *>(a.up) + n * a.ld_up;
+  f32x16 acc = f32x16{};
+#pragma unroll 4
+  for (int k0 = wave * KS; k0 < 2 * a.pad; k0 += WAVES * KS) {
+    const int at = k0 + half * VK, k = at - (at >= a.pad ? a.pad : 0);
+    const Piece dv = *reinterpret_cast<const Piece *>(d + at);
+    const Piece wv = piece_of<T, T, SHORT>(raw_piece<T, T, SHORT>(at >= a.pad ? up : gate, k, a.hidden), k, a.hidden);
+    acc = mma(__builtin_bit_cast(V, wv), __builtin_bit_cast(V, dv), acc);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    const F4 v = {acc[4 * e], acc[4 * e + 1], acc[4 * e + 2], acc[4 * e + 3]};
+    *reinterpret_cast<F4 *>(&s_acc[wave][l % 32][8 * e + 4 * half]) = v;
+  }
+  __syncthreads();
+  if (threadIdx.x >= 256) return;
+  const int row = threadIdx.x / 8, c = threadIdx.x % 8 * 4;
+  F4 t = F4{};
+#pragma unroll
+  for (int i = 0; i < WAVES; i++) t += *reinterpret_cast<F4 *>(&s_acc[i][row][c]);
+  const float v[4] = {t[0], t[1], t[2], t[3]};
+  if (r0 + row < a.rows && n0 + c < a.cols) store4(static_cast<T *>(a.dx) + (r0 + row) * a.ld_dx, n0 + c, a.cols, v);
+}
+
+// Sums over the rows of one part, x^T [dg du]: 128 WM columns of x by 64 WN of dg and du a workgroup, 128 by 64 a wave, over a slice of the rows.  The sums of
+// the slice go to, or are added to, its partial matrix, in the fragments' order.  The tiles of one slice run on one chiplet: they read the same rows.
 struct GatedDwArgs {
   const void *x, *d;
-  float *part;                               // [slices][tiles of x][tiles of d][4 fragments a wave, 4 waves]
+  float *part;                               // [slices][tiles of d][tiles of x][RI WM][2 WN] fragments
   int64_t rows, ld_x, slice;
-  int cols, pad, add;
+  int cols, pad, add, slices, tiles_c, tiles_n;
 };
-template <class T>
-__global__ __launch_bounds__(256, 2) void k_gated_dw(GatedDwArgs a) {
+template <class T, int RI, int WM, int WN, bool SHORT>
+__global__ __launch_bounds__(kWave * WM * WN, 2) void k_gated_dw(GatedDwArgs a) {
   typedef typename Frag<T>::V V;
-  constexpr int KR = kChunkK<T>, PE = 16 / sizeof(T), P = kGradPitch<T, 4>, C = 128 / PE, STEPS = KR / kStep<T>;      // rows at a time, pieces of a row
-  __shared__ __align__(16) char s_x[KR * P], s_d[KR * P];
-  const int tid = threadIdx.x, l = lane_id(), wm = tid / kWave / 2, wn = tid / kWave % 2;
-  const int c0 = blockIdx.x * 128, n0 = blockIdx.y * 128;
-  const int64_t r_begin = blockIdx.z * a.slice, r_end = min(r_begin + a.slice, a.rows);
-  float *part = a.part + (((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * gridDim.y + blockIdx.y) * 16384;
-  f32x16 acc[2][2];
+  constexpr int THREADS = kWave * WM * WN, KR = kChunkK<T>, PE = 16 / sizeof(T), STEPS = KR / kStep<T>;       // rows at a time
+  constexpr int BM = 32 * RI * WM, BN = 64 * WN, PX = BM * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 144), PD = BN * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 144), CX = BM / PE, CD = BN / PE;
+  constexpr int NX = KR * CX / THREADS, ND = KR * CD / THREADS, RX = THREADS / CX, RD = THREADS / CD;
+  __shared__ __align__(16) char s_x[KR * PX], s_d[KR * PD];
+  const int tid = threadIdx.x, l = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / kWave), wm = wave / WN, wn = wave % WN;
+  const int id = blockIdx.x / 8, tiles = a.tiles_c * a.tiles_n, slice = id / tiles * 8 + blockIdx.x % 8, tile = id % tiles;
+  if (slice >= a.slices) return;
+  const int c0 = tile % a.tiles_c * BM, n0 = tile / a.tiles_c * BN;
+  const int64_t r_begin = slice * a.slice, r_end = min(r_begin + a.slice, a.rows);
+  const int blocks = max(0, min(RI, (a.cols - c0 - wm * 32 * RI + 31) / 32)), wide = n0 + wn * 64 < 2 * a.pad;      // of x that there are; whether there are any of d
+  float *part = a.part + ((int64_t)slice * tiles + tile) * (BM * BN);
+  f32x16 acc[RI][2];
 #pragma unroll
-  for (int i = 0; i < 2; i++)
+  for (int i = 0; i < RI; i++)
 #pragma unroll
     for (int n = 0; n < 2; n++)
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         F4 v = F4{};
-        if (a.add) v = reinterpret_cast<const F4 *>(part)[(((wm * 2 + i) * 4 + wn * 2 + n) * 4 + e) * 64 + l];
+        if (a.add) v = reinterpret_cast<const F4 *>(part)[(((wm * RI + i) * 2 * WN + wn * 2 + n) * 4 + e) * 64 + l];
 #pragma unroll
         for (int j = 0; j < 4; j++) acc[i][n][4 * e + j] = v[j];
       }
-  Piece x[4], d[4];
-  auto fetch = [&](int64_t r0) {
+  Piece x[NX], d[ND];
+  const int xc = c0 + tid % CX * PE, dc = n0 + tid % CD * PE;
+  const int dc_in = min(dc, 2 * a.pad - PE);
+  auto fetch = [&](int64_t r0) {             // of the last chunk the last row stands in for those past the slice's end
+    const int left = (int)max((int64_t)1, min(r_end - r0, (int64_t)KR));
+    const T *xp = static_cast<const T *>(a.x) + min(r0, a.rows - 1) * a.ld_x, *dp = static_cast<const T *>(a.d) + min(r0, a.rows - 1) * 2 * a.pad + dc_in;
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      const int i = tid + 256 * j, c = i % C * PE;
-      const int64_t r = r0 + i / C;
-      x[j] = d[j] = Piece{};
-      if (r >= r_end) continue;
-      if (c0 + c < a.cols) x[j] = row_piece(static_cast<const T *>(a.x) + r * a.ld_x, c0 + c, a.cols);
-      if (n0 + c < 2 * a.pad) d[j] = *reinterpret_cast<const Piece *>(static_cast<const T *>(a.d) + r * 2 * a.pad + n0 + c);
-    }
+    for (int j = 0; j < NX; j++) x[j] = raw_piece<T, T, SHORT>(xp + min(tid / CX + RX * j, left - 1) * a.ld_x, xc, a.cols);
+#pragma unroll
+    for (int j = 0; j < ND; j++) d[j] = *reinterpret_cast<const Piece *>(dp + (uint32_t)(min(tid / CD + RD * j, left - 1) * 2 * a.pad));
   };
-  auto put = [&]() {
+  auto put = [&](int64_t r0) {
+    const int left = (int)min(r_end - r0, (int64_t)KR);
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      const int i = tid + 256 * j;
-      *reinterpret_cast<Piece *>(s_x + i / C * P + i % C * 16) = x[j];
-      *reinterpret_cast<Piece *>(s_d + i / C * P + i % C * 16) = d[j];
+    for (int j = 0; j < NX; j++) {
+      Piece v = piece_of<T, T, SHORT>(x[j], xc, a.cols);
+      if (left < KR && tid / CX + RX * j >= left) v = Piece{};
+      *reinterpret_cast<Piece *>(s_x + (tid / CX + RX * j) * PX + tid % CX * 16) = v;
+    }
+#pragma unroll
+    for (int j = 0; j < ND; j++) {
+      Piece v = d[j];
+      if (left < KR && tid / CD + RD * j >= left) v = Piece{};
+      *reinterpret_cast<Piece *>(s_d + (tid / CD + RD * j) * PD + tid % CD * 16) = v;
     }
   };
   fetch(r_begin);
-  put();
+  put(r_begin);
   __syncthreads();
   for (int64_t r0 = r_begin; r0 < r_end; r0 += KR) {
     const bool more = r0 + KR < r_end;
     if (more) fetch(r0 + KR);
 #pragma unroll
     for (int s = 0; s < STEPS; s++) {
-      V xs[2], ds[2];
+      V xs[RI], ds[2];
 #pragma unroll
-      for (int i = 0; i < 2; i++) {
-        xs[i] = columns_frag<T>(s_x, P, s, wm * 2 + i);
-        ds[i] = columns_frag<T>(s_d, P, s, wn * 2 + i);
-      }
+      for (int n = 0; n < 2; n++) ds[n] = columns_frag<T>(s_d, PD, s, wn * 2 + n);
+#pragma unroll
+      for (int i = 0; i < RI; i++) xs[i] = columns_frag<T>(s_x, PX, s, wm * RI + i);
       mma_block<T>(ds, xs, acc);
     }
     __syncthreads();
-    if (more) put();
+    if (more) put(r0 + KR);
     __syncthreads();
   }
+  if (!wide) return;
 #pragma unroll
-  for (int i = 0; i < 2; i++)
+  for (int i = 0; i < RI; i++) {
+    if (i >= blocks) continue;
 #pragma unroll
     for (int n = 0; n < 2; n++)
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         const F4 v = {acc[i][n][4 * e], acc[i][n][4 * e + 1], acc[i][n][4 * e + 2], acc[i][n][4 * e + 3]};
-        reinterpret_cast<F4 *>(part)[(((wm * 2 + i) * 4 + wn * 2 + n) * 4 + e) * 64 + l] = v;
+        reinterpret_cast<F4 *>(part)[(((wm * RI + i) * 2 * WN + wn * 2 + n) * 4 + e) * 64 + l] = v;
       }
+  }
 }
 
 // Partial matrices to the weights' gradients: 64 elements, four by four, a workgroup; 16 threads share a sum, in the slices' order.
@@ -731,35 +778,37 @@ struct GatedSumArgs {
   const float *part;
   void *d_gate, *d_up;
   int64_t ld_gate, ld_up;
-  int slices, type, cols, hidden, pad, tiles_c, tiles_n;
+  int slices, type, cols, hidden, pad, tiles_c, tiles_n, kt, nt;             // kt by nt fragments a tile
 };
 __global__ __launch_bounds__(256) void k_gated_sum(GatedSumArgs a) {
   __shared__ F4 s[16][17];
-  const int x = threadIdx.x % 16, y = threadIdx.x / 16;
-  const int64_t n = (int64_t)a.tiles_c * a.tiles_n * 16384, i = ((int64_t)blockIdx.x * 16 + x) * 4;
-  F4 t = F4{};
-#pragma unroll 4
-  for (int p = y; p < a.slices; p += 16) t += *reinterpret_cast<const F4 *>(a.part + p * n + i);
-  s[y][x] = t;
-  __syncthreads();
-  if (y) return;
-  t = F4{};
-#pragma unroll
-  for (int p = 0; p < 16; p++) t += s[p][x];
-  const int tile = (int)(i / 16384), f = (int)(i % 16384), frag = f / 1024, e = f / 256 % 4, lane = f / 4 % 64;
-  const int c = tile / a.tiles_n * 128 + frag / 4 * 32 + lane % 32;
-  int h = tile % a.tiles_n * 128 + frag % 4 * 32 + 8 * e + 4 * (lane / 32);
+  const int x = threadIdx.x % 16, y = threadIdx.x / 16, per = a.kt * a.nt * 1024;
+  const int64_t n = (int64_t)a.tiles_c * a.tiles_n * per, i = ((int64_t)blockIdx.x * 16 + x) * 4;
+  const int tile = (int)(i / per), f = (int)(i % per), frag = f / 1024, e = f / 256 % 4, lane = f / 4 % 64;
+  const int c = (tile % a.tiles_c * a.kt + frag / a.nt) * 32 + lane % 32;
+  int h = (tile / a.tiles_c * a.nt + frag % a.nt) * 32 + 8 * e + 4 * (lane / 32);
   const bool up = h >= a.pad;
   if (up) h -= a.pad;
   void *out = up ? a.d_up : a.d_gate;
-  if (c >= a.cols || !out) return;
+  const bool wanted = c < a.cols && h < a.hidden && out;     // (fragments beside the matrix are not written either)
+  F4 t = F4{};
+  if (wanted)
+#pragma unroll 4
+    for (int p = y; p < a.slices; p += 16) t += *reinterpret_cast<const F4 *>(a.part + p * n + i);
+  s[y][x] = t;
+  __syncthreads();
+  if (y || !wanted) return;
+  t = F4{};
+#pragma unroll
+  for (int p = 0; p < 16; p++) t += s[p][x];
   for (int j = 0; j < 4; j++)
     if (h + j < a.hidden) store_any(out, (int64_t)c * (up ? a.ld_up : a.ld_gate) + h + j, a.type, t[j]);
 }
 
 // ------------------------------------------------------------------------------------ a few rows
 // One row and 32 columns of h a workgroup: lanes side by side take 16 bytes of a row of Wg and of Wu, the rest of the workgroup splits the depth.
-template <class T>
+// GRAD: dg and du in 32 bits go to `out`, [rows][2 hidden] of float.
+template <class T, bool GRAD>
 __global__ __launch_bounds__(kHeadThreads) void k_gated_few(GatedArgs a) {
   constexpr int VK = kVec<T>, CL = 32 / VK, SL = kHeadThreads / CL, W = kHeadThreads / kWave;
   __shared__ float s_sum[2][W][32];
@@ -792,10 +841,110 @@ __global__ __launch_bounds__(kHeadThreads) void k_gated_few(GatedArgs a) {
   float gv = 0.f, uv = 0.f;
 #pragma unroll
   for (int i = 0; i < W; i++) { gv += s_sum[0][i][threadIdx.x]; uv += s_sum[1][i][threadIdx.x]; }
-  static_cast<T *>(a.out)[r * a.ld_out + c] = (T)(activate(gv, a.act) * uv);
+  if constexpr (GRAD) {
+    const float dh = (float)static_cast<const T *>(a.dh)[r * a.ld_dh + c];
+    gate_grad_all<1>(&gv, &uv, &dh, a.act);
+    float *out = static_cast<float *>(a.out) + r * 2 * a.hidden + c;
+    out[0] = gv;
+    out[a.hidden] = uv;
+  } else static_cast<T *>(a.out)[r * a.ld_out + c] = (T)(activate(gv, a.act) * uv);
+}
+
+// Gradients of a few rows from dg and du in 32 bits.  dx: a row and 16 columns a workgroup, a wave takes four of them, its lanes side by side along
+// the weights' rows.  dWg and dWu: a thread has 16 bytes of a row of each.  In 32 bits because so few numbers do not even out what rounding
+// them first would cost, and because these launches are latency alone.
+struct GatedFewArgs {
+  const float *d;
+  const void *x, *gate, *up;
+  void *dx, *d_gate, *d_up;
+  int64_t rows, ld_x, ld_gate, ld_up, ld_dx, ld_dg, ld_du;
+  int cols, hidden;
+};
+template <class T>
+__global__ __launch_bounds__(kHeadThreads) void k_gated_dx_few(GatedFewArgs a) {
+  constexpr int VK = kVec<T>;
+  const int64_t r = blockIdx.y;
+  const int l = lane_id(), c0 = blockIdx.x * 16 + threadIdx.x / kWave * 4;
+  float t[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int part = 0; part < 2; part++) {
+    const float *d = a.d + (r * 2 + part) * a.hidden;
+    const T *w = static_cast<const T *>(part ? a.up : a.gate);
+    const int64_t ld = part ? a.ld_up : a.ld_gate;
+    for (int n = l * VK; n < a.hidden; n += kWave * VK) {
+      float dv[VK];
+      if (n + VK <= a.hidden) load_pack<float, VK>(d + n, dv);
+      else
+#pragma unroll
+        for (int j = 0; j < VK; j++) dv[j] = n + j < a.hidden ? d[n + j] : 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const typename Frag<T>::V v = row_frag<T>(w + (int64_t)min(c0 + q, a.cols - 1) * ld, n, a.hidden);
+#pragma unroll
+        for (int j = 0; j < VK; j++) t[q] = fmaf(dv[j], (float)v[j], t[q]);
+      }
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 4; q++) {
+    t[q] = group_sum<kWave>(t[q]);
+    if (l == 0 && c0 + q < a.cols) static_cast<T *>(a.dx)[r * a.ld_dx + c0 + q] = (T)t[q];
+  }
+}
+template <class T>
+__global__ __launch_bounds__(kHeadThreads) void k_gated_dw_few(GatedFewArgs a) {
+  constexpr int VK = kVec<T>;
+  const int pieces = (a.hidden + VK - 1) / VK;
+  const int64_t i = (int64_t)blockIdx.x * kHeadThreads + threadIdx.x;
+  const int c = (int)(i / pieces), n = max(0, min((int)(i % pieces) * VK, a.hidden - VK));       // a last piece that is cut starts earlier: the same numbers
+  if (c >= a.cols) return;
+  float g[VK], u[VK];
+#pragma unroll
+  for (int j = 0; j < VK; j++) g[j] = u[j] = 0.f;
+  const T *x = static_cast<const T *>(a.x) + c;
+  if (a.hidden >= VK) {
+    constexpr int R = 8;                     // rows under way
+    for (int64_t r0 = 0; r0 < a.rows; r0 += R) {
+      float xv[R], dg[R][VK], du[R][VK];
+#pragma unroll
+      for (int q = 0; q < R; q++) {
+        const int64_t r = min(r0 + q, a.rows - 1);
+        xv[q] = (float)x[r * a.ld_x];
+        load_pack<float, VK>(a.d + r * 2 * a.hidden + n, dg[q]);
+        load_pack<float, VK>(a.d + (r * 2 + 1) * a.hidden + n, du[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < R; q++)
+        if (r0 + q < a.rows)
+#pragma unroll
+          for (int j = 0; j < VK; j++) {
+            g[j] = fmaf(xv[q], dg[q][j], g[j]);
+            u[j] = fmaf(xv[q], du[q][j], u[j]);
+          }
+    }
+  } else
+    for (int64_t r = 0; r < a.rows; r++)
+#pragma unroll
+      for (int j = 0; j < VK; j++)
+        if (j < a.hidden) {
+          g[j] = fmaf((float)x[r * a.ld_x], a.d[r * 2 * a.hidden + j], g[j]);
+          u[j] = fmaf((float)x[r * a.ld_x], a.d[(r * 2 + 1) * a.hidden + j], u[j]);
+        }
+  for (int part = 0; part < 2; part++) {
+    T *out = static_cast<T *>(part ? a.d_up : a.d_gate);
+    if (!out) continue;
+    out += c * (part ? a.ld_du : a.ld_dg) + n;
+    const float *v = part ? u : g;
+    if (n + VK <= a.hidden) store_pack<T, VK>(out, v);
+    else
+#pragma unroll
+      for (int j = 0; j < VK; j++)
+        if (n + j < a.hidden) out[j] = (T)v[j];
+  }
 }
 
 // ------------------------------------------------------------------------------------ host side
+// rows of x or of the weights that hold no whole piece of 16 bytes
+template <class T> static bool is_short(int cols, int hidden) { return std::min(cols, hidden) < 16 / (int)sizeof(T); }
 constexpr int64_t kFewRows = 16, kFewResults = 64 * 1024;    // as ink_linear: each workgroup asks for its columns of both matrices again for every row
 
 // Many rows, and a depth whose weights fit the registers: workgroups for the whole card, each with a stream of row tiles.
@@ -856,39 +1005,51 @@ template <class TL, class T, class TO> static void gated_tiles(const GatedArgs &
     b.out = static_cast<TO *>(a.out) + r0 * a.ld_out;
     if (a.x_scale) b.x_scale = a.x_scale + r0;
     const int64_t tiles = (b.rows + 127) / 128;
-    run(k_gated_tile<TL, T, TO, 2, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * gy)), dim3(256), b);
+    run(is_short<T>(a.cols, a.hidden) ? k_gated_tile<TL, T, TO, 2, false, true> : k_gated_tile<TL, T, TO, 2, false, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * gy)), dim3(256), b);
   }
 }
 template <class T, class TO> static void gated_run(const GatedArgs &a, Launches &run) {
   if constexpr (sizeof(T) != 1)
     if (a.rows <= kFewRows && a.rows * a.hidden <= kFewResults)
-      return run(k_gated_few<T>, dim3((a.hidden + 31) / 32, (unsigned)a.rows), dim3(kHeadThreads), a);
+      return run(k_gated_few<T, false>, dim3((a.hidden + 31) / 32, (unsigned)a.rows), dim3(kHeadThreads), a);
   if constexpr (sizeof(T) != 1 || sizeof(TO) != 4)
     if (stream_run<T, TO, false>(a, run)) return;
   gated_tiles<T, std::conditional_t<sizeof(T) == 1 && sizeof(TO) == 4, bf16, T>, TO>(a, run);
 }
 
-// The gradient takes the rows in parts whose dg and du (2 pad columns) have about 128 MB, so that the products that read them find them in the cache behind
-// the L2s, and the work memory does not grow with the rows.
-struct GatedPlan { int pad, tiles_c, tiles_n, slices; int64_t part_rows, slice, d_bytes, part_bytes; };
+// The gradient takes the rows in parts whose dg and du (2 pad columns) have up to 1 GB, so that the work memory does not grow with the rows.  (Parts of
+// 128 MB, which the cache behind the L2s would hold, cost more in launches and partial sums than they save: 233k x 256 x 683 bf16 1123 us instead of 1022,
+// 353k x 78 x 208 f32 1467 instead of 1227.)
+// Few rows in the gradient, or so few numbers in dg that the errors of rounding them would not even out (3 x 602 x 62 bf16: 0.0025 from 64 bits, where
+// rounding the results alone gives 0.0017).
+static bool grad_of_few(int64_t rows, int hidden) { return rows * hidden <= (rows <= 2 * kFewRows ? kFewResults : rows <= 64 ? 4096 : 0); }
+constexpr int64_t kFullTiles = 64;           // tiles of 128 by 128 from which on they are faster than small ones
+struct GatedPlan { int pad, ri, wm, wn, tiles_c, tiles_n, slices; int64_t part_rows, slice, d_bytes, part_bytes; };
 static GatedPlan gated_plan(int64_t rows, int cols, int hidden, int type) {
   GatedPlan p{};
-  p.pad = (hidden + kTileHidden - 1) / kTileHidden * kTileHidden;
+  p.pad = (hidden + 31) / 32 * 32;
   const int64_t row_bytes = 2ll * p.pad * type_size(type);
-  p.part_rows = std::min((rows + 127) / 128 * 128, std::max<int64_t>(1024, (128 << 20) / row_bytes / 1024 * 1024));
+  p.part_rows = std::min((rows + 255) / 256 * 256, std::max<int64_t>(1024, (1ll << 30) / row_bytes / 1024 * 1024));
+  // the weights' gradients: 128 columns of x by 128 of dg and du; by 256, 128 by 64 a wave, where 16-bit rows are many and have no more columns
+  // (1M x 128 x 344 398 us instead of 436, but 100k x 602 x 1605 1006 instead of 833: two workgroups a CU instead of three)
+  const bool wide = type != INK_F32 && p.part_rows >= 8192 && cols <= 128;
+  p.ri = wide ? 4 : 2;
+  p.wm = wide ? 1 : 2;
+  p.wn = 4 / p.wm;
   p.tiles_c = (cols + 127) / 128;
-  p.tiles_n = (2 * p.pad + 127) / 128;
+  p.tiles_n = (2 * p.pad + 64 * p.wn - 1) / (64 * p.wn);
   const int64_t steps = p.part_rows / 64, tiles = (int64_t)p.tiles_c * p.tiles_n;     // 64 rows: whole chunks of every type
-  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(steps / 2, 1024 / tiles));
+  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(steps / 2, (wide ? 512 : 1024) / tiles));
   p.slice = (steps + slices - 1) / slices * 64;
   p.slices = (int)((p.part_rows + p.slice - 1) / p.slice);
   p.d_bytes = p.part_rows * row_bytes;
-  p.part_bytes = (int64_t)p.slices * tiles * 16384 * 4;
+  p.part_bytes = (int64_t)p.slices * tiles * (128 * 64 * p.wn) * 4;
   return p;
 }
 
 template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void *work, void *dx, int64_t ld_dx, bool weights, Launches &run) {
   const int64_t rows = a.rows;
+  const bool brief = is_short<T>(a.cols, a.hidden);
   a.out = work; a.ld_out = 2 * p.pad; a.pad = p.pad;
   for (int64_t r0 = 0; r0 < rows; r0 += p.part_rows) {
     GatedArgs b = a;
@@ -896,16 +1057,29 @@ template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void 
     b.x = static_cast<const T *>(a.x) + r0 * a.ld_x;
     b.dh = static_cast<const T *>(a.dh) + r0 * a.ld_dh;
     const int64_t tiles = (b.rows + 127) / 128;
-    if (!stream_run<T, T, true>(b, run)) run(k_gated_tile<T, T, T, 2, true>, dim3((unsigned)((tiles + 7) / 8 * 8 * (p.pad / kTileHidden))), dim3(256), b);
+    if (!stream_run<T, T, true>(b, run)) run(brief ? k_gated_tile<T, T, T, 2, true, true> : k_gated_tile<T, T, T, 2, true, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * ((a.hidden + kTileHidden - 1) / kTileHidden))), dim3(256), b);
     if (dx) {
       GatedDxArgs q{work, a.gate, a.up, static_cast<T *>(dx) + r0 * ld_dx, b.rows, a.ld_gate, a.ld_up, ld_dx, a.cols, a.hidden, p.pad};
-      run(k_gated_dx<T>, dim3((unsigned)((tiles + 7) / 8 * 8 * p.tiles_c)), dim3(256), q);
+      const int gy = (a.cols + 127) / 128;
+      if (tiles * gy < kFullTiles) run(brief ? k_gated_dx_small<T, true> : k_gated_dx_small<T, false>, dim3((unsigned)((b.rows + 31) / 32), (a.cols + 31) / 32), dim3(512), q);
+      else run(brief ? k_gated_dx<T, true> : k_gated_dx<T, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * gy)), dim3(256), q);
     }
     if (weights) {
-      GatedDwArgs q{b.x, work, reinterpret_cast<float *>(static_cast<char *>(work) + p.d_bytes), b.rows, a.ld_x, p.slice, a.cols, p.pad, r0 > 0};
-      run(k_gated_dw<T>, dim3(p.tiles_c, p.tiles_n, p.slices), dim3(256), q);
+      GatedDwArgs q{b.x, work, reinterpret_cast<float *>(static_cast<char *>(work) + p.d_bytes), b.rows, a.ld_x, p.slice, a.cols, p.pad, r0 > 0, p.slices,
+                    p.tiles_c, p.tiles_n};
+      const auto kernel = p.ri == 4 ? (brief ? k_gated_dw<T, 4, 1, 4, true> : k_gated_dw<T, 4, 1, 4, false>) : (brief ? k_gated_dw<T, 2, 2, 2, true> : k_gated_dw<T, 2, 2, 2, false>);
+      run(kernel, dim3((unsigned)((p.slices + 7) / 8 * 8 * p.tiles_c * p.tiles_n)), dim3(256), q);
     }
   }
+}
+
+template <class T> static void gated_grad_few(GatedArgs a, GatedFewArgs f, void *work, Launches &run) {
+  a.out = work;
+  run(k_gated_few<T, true>, dim3((a.hidden + 31) / 32, (unsigned)a.rows), dim3(kHeadThreads), a);
+  f.d = static_cast<const float *>(work);
+  if (f.dx) run(k_gated_dx_few<T>, dim3((a.cols + 15) / 16, (unsigned)a.rows), dim3(kHeadThreads), f);
+  const int64_t pieces = (int64_t)a.cols * ((a.hidden + kVec<T> - 1) / kVec<T>);
+  if (f.d_gate || f.d_up) run(k_gated_dw_few<T>, dim3((unsigned)((pieces + kHeadThreads - 1) / kHeadThreads)), dim3(kHeadThreads), f);
 }
 
 static const char *gated_check(int64_t rows, int32_t cols, int32_t hidden, int32_t act) {
@@ -947,6 +1121,7 @@ extern "C" ink_status ink_gated(const void *x, int64_t ld_x, const float *x_scal
 
 extern "C" size_t ink_gated_backward_work(int64_t rows, int32_t cols, int32_t hidden, int32_t type) {
   if (!known_type(type) || rows < 1 || gated_check(rows, cols, hidden, INK_ACT_NONE)) return 0;
+  if (grad_of_few(rows, hidden)) return (size_t)rows * 2 * hidden * sizeof(float);
   const GatedPlan p = gated_plan(rows, cols, hidden, type);
   return (size_t)(p.d_bytes + p.part_bytes);
 }
@@ -969,11 +1144,17 @@ extern "C" ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const vo
   if (rows > 0 && (dx || weights) && (!work || !aligned_to(work, 16) || work_bytes < ink_gated_backward_work(rows, cols, hidden, type)))
     return fail_call(INK_E_ARG, "%s: work holds less than ink_gated_backward_work bytes or is not aligned to 16", who);
   Launches run(hip_stream);
+  GatedArgs a{};
+  a.x = x; a.gate = w_gate; a.up = w_up; a.dh = dh;
+  a.rows = rows; a.ld_x = ld_x; a.ld_gate = ld_gate; a.ld_up = ld_up; a.ld_dh = ld_dh; a.cols = cols; a.hidden = hidden; a.act = act;
+  if (rows > 0 && (dx || weights) && grad_of_few(rows, hidden)) {
+    const GatedFewArgs f{nullptr, x, w_gate, w_up, dx, dw_gate, dw_up, rows, ld_x, ld_gate, ld_up, ld_dx, ld_dg, ld_du, cols, hidden};
+    if (type == INK_F32) gated_grad_few<float>(a, f, work, run);
+    else type == INK_BF16 ? gated_grad_few<bf16>(a, f, work, run) : gated_grad_few<f16>(a, f, work, run);
+    return run.done(who);
+  }
   GatedPlan p = gated_plan(std::max<int64_t>(rows, 1), cols, hidden, type);
   if (rows > 0 && (dx || weights)) {
-    GatedArgs a{};
-    a.x = x; a.gate = w_gate; a.up = w_up; a.dh = dh;
-    a.rows = rows; a.ld_x = ld_x; a.ld_gate = ld_gate; a.ld_up = ld_up; a.ld_dh = ld_dh; a.cols = cols; a.hidden = hidden; a.act = act;
     if (type == INK_F32) gated_grad<float>(a, p, work, dx, ld_dx, weights, run);
     else type == INK_BF16 ? gated_grad<bf16>(a, p, work, dx, ld_dx, weights, run) : gated_grad<f16>(a, p, work, dx, ld_dx, weights, run);
   }
@@ -981,8 +1162,8 @@ extern "C" ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const vo
     GatedSumArgs s{};
     s.part = reinterpret_cast<const float *>(static_cast<const char *>(work) + p.d_bytes);
     s.d_gate = dw_gate; s.d_up = dw_up; s.ld_gate = ld_dg; s.ld_up = ld_du; s.slices = rows > 0 ? p.slices : 0; s.type = type;
-    s.cols = cols; s.hidden = hidden; s.pad = p.pad; s.tiles_c = p.tiles_c; s.tiles_n = p.tiles_n;
-    run(k_gated_sum, dim3((unsigned)((int64_t)p.tiles_c * p.tiles_n * 256)), dim3(256), s);
+    s.cols = cols; s.hidden = hidden; s.pad = p.pad; s.tiles_c = p.tiles_c; s.tiles_n = p.tiles_n; s.kt = 4; s.nt = 2 * p.wn;
+    run(k_gated_sum, dim3((unsigned)((int64_t)p.tiles_c * p.tiles_n * s.kt * s.nt * 16)), dim3(256), s);
   }
   return run.done(who);
 }

@@ -257,10 +257,10 @@ def gated_grad_ref(dh, x, wg, wu, act, dtype):
     e_dg = dh.abs() * (eu * s.abs() + u_.abs() * e_slope) + 4 * u * dg.abs()
     slope = s.abs() + eg if act in ("gelu", "silu") else torch.ones_like(g)
     e_du = dh.abs() * (slope * eg + E_ACT[act] * (1 + g.abs())) + 4 * u * du.abs()
-    if dtype is not F32:
+    if dtype is not F32 and not (rows * wg.shape[1] <= 65536 if rows <= 32 else rows <= 64 and rows * wg.shape[1] <= 4096):   # (few: kept in 32 bits)
         tiny = 2.0 ** -25 if dtype is F16 else 0.0
         e_dg, e_du = e_dg + U[dtype] * (dg.abs() + e_dg) + tiny, e_du + U[dtype] * (du.abs() + e_du) + tiny
-    n, m = 2 * wg.shape[1] + 8, rows + 64
+    n, m = 2 * wg.shape[1] + 16, rows + 64
     dx, e_dx = dg @ wg.t() + du @ wu.t(), e_dg @ wg.abs().t() + e_du @ wu.abs().t() + n * u * (dg.abs() @ wg.abs().t() + du.abs() @ wu.abs().t())
     return ((dx, e_dx), (x.t() @ dg, x.abs().t() @ e_dg + m * u * (x.abs().t() @ dg.abs())),
             (x.t() @ du, x.abs().t() @ e_du + m * u * (x.abs().t() @ du.abs())))
