@@ -11,6 +11,7 @@ Tensors of other devices or types and shapes that do not fit raise.
 import array
 import ctypes as C
 import itertools
+import operator
 
 import torch
 
@@ -413,12 +414,13 @@ def adamw_moments(params, bits=32):
 
 
 _numel, _address, _contiguous, _device_index = torch.Tensor.numel, torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
+_dtype, _shape, _requires_grad = operator.attrgetter("dtype"), operator.attrgetter("shape"), operator.attrgetter("requires_grad")
 
 
 def _held(ts, name, sizes, dev, dtypes):
     """Addresses of the tensors that a step changes in place: contiguous, of these numbers of elements, on the GPU `dev`.  All of a list at
     a time: a head has hundreds of tensors, and a call should take less than the step."""
-    types = {t.dtype for t in ts}
+    types = set(map(_dtype, ts))
     if not types <= dtypes:
         raise TypeError("%s has type %s, wanted %s" % (name, (types - dtypes).pop(), " or ".join(sorted(map(str, dtypes)))))
     if set(map(_device_index, ts)) != {dev}:
@@ -454,15 +456,15 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
     if dev < 0:
         raise ValueError("params must be GPU tensors")
     width = len(mom[0])
-    if width not in (2, 4) or any(len(m) != width for m in mom):
+    if width not in (2, 4) or set(map(len, mom)) != {width}:
         raise ValueError("moments must be adamw_moments', all of one width")
     sizes = list(map(_numel, p))
     at = _held(p, "a parameter", sizes, dev, _PARAMS)
-    if any(x.requires_grad and not x.is_leaf for x in p) and torch.is_grad_enabled():
+    if any(map(_requires_grad, p)) and torch.is_grad_enabled() and not all(x.is_leaf for x in p):
         raise ValueError("a parameter that requires a gradient and is no leaf cannot be changed in place")
-    if not {x.dtype for x in g} <= TYPES.keys() or set(map(_device_index, g)) != {dev} or any(x.shape != y.shape for x, y in zip(g, p)):
+    if not set(map(_dtype, g)) <= TYPES.keys() or set(map(_device_index, g)) != {dev} or list(map(_shape, g)) != list(map(_shape, p)):
         raise ValueError("a gradient must be a float32, bfloat16 or float16 tensor of its parameter's shape, on its GPU")
-    if any(x.requires_grad for x in g):
+    if any(map(_requires_grad, g)):
         _unrecorded(g, "a gradient")
     if not all(map(_contiguous, g)):
         g = [x.contiguous() for x in g]
@@ -473,7 +475,7 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
         held = [_held([m[0] for m in mom], "a first moment", sizes, dev, _CODES), _held([m[1] for m in mom], "a scale of first moments", blocks, dev, _SCALES),
                 _held([m[2] for m in mom], "a second moment", sizes, dev, _CODES), _held([m[3] for m in mom], "a scale of second moments", blocks, dev, _SCALES)]
     none = [0] * n
-    c, here, copy = none, [], [None] * n
+    c, here, copy = none, [], none
     if copies is not None:
         copy = [copies[i] for i in place] if some else copies
         here = [i for i in range(n) if copy[i] is not None]
@@ -483,8 +485,10 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
             c = list(none)
             for i, x in zip(here, _held([copy[i] for i in here], "a copy", [sizes[i] for i in here], dev, _COPIES)):
                 c[i] = x
-    # (tensors without elements have no address of their own)
-    changed = [x for column in (at, *held, c) if column is not None and column is not none for x, s in zip(column, sizes) if s and x]
+    changed = [x for column in (at, *held, c) if column for x in column]
+    if not all(sizes):                                                        # tensors without elements have no address of their own
+        changed = [x for column in (at, *held, c) if column for x, size in zip(column, sizes) if size]
+    changed = [x for x in changed if x] if len(here) < n else changed        # (no copy: 0)
     if len(set(changed)) != len(changed):
         raise ValueError("a tensor that the step changes stands in the call twice")
     step_at = scale_at = None
@@ -500,12 +504,13 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
         scale_at, grad_scale = grad_scale.data_ptr(), 1.0
     lib = _functions()
     entries = list(zip(at, map(_address, g), c, held[0], held[2], held[1] or none, held[3] or none, sizes, place))
-    kinds = [(x.dtype, y.dtype, None if z is None else z.dtype) for x, y, z in zip(p, g, copy)]
+    kinds = list(zip(map(_dtype, p), map(_dtype, g), [None if x is None else x.dtype for x in copy] if here else none))
     for kind in dict.fromkeys(kinds):
-        table = array.array("q", itertools.chain.from_iterable(e for e, k in zip(entries, kinds) if k == kind))
+        mine = [e for e, k in zip(entries, kinds) if k == kind]
+        table = array.array("q", itertools.chain.from_iterable(mine))
         tp, tg, tc = kind
-        _call(lib.ink_adamw, like, table.buffer_info()[0], len(table) // 9, TYPES[tp], TYPES[tg], -1 if tc is None else TYPES[tc], 8 if width == 4 else 32, lr,
-              betas[0], betas[1], eps, weight_decay, step, step_at, grad_scale, scale_at, seed & 0xFFFFFFFFFFFFFFFF)
+        _call(lib.ink_adamw, like, table.buffer_info()[0], len(mine), TYPES[tp], TYPES[tg], TYPES[tc] if tc else -1, 8 if width == 4 else 32, lr, betas[0], betas[1],
+              eps, weight_decay, step, step_at, grad_scale, scale_at, seed & 0xFFFFFFFFFFFFFFFF)
     # what autograd has kept of these tensors is no longer what they hold
     torch.autograd.graph.increment_version(p)
     if here:
