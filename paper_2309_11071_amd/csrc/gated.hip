@@ -3,6 +3,22 @@
 //   forward   g = x Wg, u = x Wu (8-bit rows and weights: times the row's and the column's scale),  h = act(g) u
 //   gradient  g and u formed anew from x;  dg = dh u act'(g), du = dh act(g);
 //             dx = dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du
+//
+// As in linear.hip every product is formed transposed, the weights' columns as the instruction's rows, so that a lane ends up with four
+// neighbouring columns of its row, here of g and of u: act(g) u needs nothing of another lane.  Which kernel, forward:
+//
+//   up to 16 rows, 64k results   k_gated_few     a row and 32 columns a workgroup; the weights are what is read: 1 x 256 x 683 bf16 6 us
+//   from 16384 or 32768 rows on  k_gated_stream  the weights in registers, rows in a stream; depths of up to 256 (16 bits), 128 (32 bits) or 512 (8 bits)
+//   else                         k_gated_tile    128 rows by 64 columns, both operands through LDS
+//
+// What bounds the stream: reading rows and writing h (16 bits, 128 columns), the vector instructions of the activation (8 bits, whose products take a
+// quarter of the time), the matrix unit (32 bits).  Figures at each kernel.
+//
+// The gradient does not keep g and u: forming them again costs 4 rows cols hidden operations, keeping them 8 bytes an element of h written and
+// read (1M x 128 x 344 bf16: 0.16 ms of the matrix unit against 0.55 ms of memory).  dg and du are left in work memory once, in the rows' type, for the two
+// products that read them: an error of the size of the results' own rounding (233k x 256 x 683 bf16 0.0024 from 64 bits where rounding the results alone
+// gives 0.0017).  A few rows are kept in 32 bits.  The weights' gradients are sums over all rows: workgroups take slices of the rows and leave a
+// partial matrix each, added up in order (no atomics: the same call gives the same bits).
 #include <algorithm>
 #include <type_traits>
 
@@ -151,7 +167,10 @@ template <int N> __device__ __forceinline__ void gate_grad_all(float g[N], float
 }
 
 // ------------------------------------------------------------------------------------ tiles
-// 64 RB rows by 64 columns of h a workgroup, 32 RB by 32 a wave (a tile of Wg and one of Wu, so that g and u of an element meet in a lane).
+// 64 RB rows by 64 columns of h a workgroup, 32 RB by 32 a wave (a tile of Wg and one of Wu, so that g and u of an element meet in a lane), 128 bytes
+// of the depth at a time: while one piece is multiplied the next is on its way in registers.  16-bit weights lie in LDS as they do in memory, and the
+// transposing read makes fragments of their columns.  100k x 602 x 1605 bf16 700 us (550 TFLOP/s), which LDS bounds: a wave reads 4 KB of it for four
+// products of 32 cycles.
 // TL: type of the operands in memory, T: in the products, TO: of h.  GRAD: dg and du go to `out` in place of h.
 template <class TL, class T, class TO, int RB, bool GRAD, bool SHORT>
 __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
@@ -317,18 +336,17 @@ __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
 
 // ------------------------------------------------------------------------------------ many rows
 // Rows in a stream past weights in registers: a wave has the fragments of 32 columns of Wg and of Wu over the whole depth (KS steps) for good, a
-// workgroup WN waves side by side and WM below each other.  It takes 32 RB WM rows at a time; all threads load them side by side, a
+// workgroup WN waves side by side and WM below each other.  It takes 32 WM rows at a time; all threads load them side by side, a
 // tile ahead, into one of two buffers in LDS, from where every wave reads the fragments of its rows: one barrier a tile.  The results
 // turn in LDS that is the wave's own, from four columns a lane to 64 bytes of a row side by side, so no wave waits for another's activations.  The
 // next tile's rows go into LDS before this tile's results are stored: memory answers in order, so a wait for rows asked for is one for all
 // stores before them, and those of the tile before have had the products' time (2.45M x 128 x 344 bf16: 812 us with the stores first).
 struct StreamPlan { int groups, row_groups; };               // workgroups side by side, and below each other
-template <class T, int KS, int WM> constexpr int stream_blocks() { return WM > 1 || KS * kTypeStep<T> * (int)sizeof(T) > 256 || sizeof(T) == 2 ? 1 : 2; }
 template <class T, class TO, int KS, int WN, int WM, int PER, bool GRAD>
 __global__ __launch_bounds__(kWave * WN * WM, PER) void k_gated_stream(GatedArgs a, StreamPlan plan) {
   typedef typename Frag<T>::V V;
   constexpr bool DEEP = sizeof(T) != 1;
-  constexpr int THREADS = kWave * WN * WM, RB = stream_blocks<T, KS, WM>(), MR = 32 * RB * WM;
+  constexpr int THREADS = kWave * WN * WM, MR = 32 * WM;
   constexpr int KB = KS * kTypeStep<T> * (int)sizeof(T), P = KB + 16;        // bytes of a row, and between rows in LDS
   constexpr int PE = 16 / sizeof(T), ROWS = THREADS / (KB / 16), NL = (MR + ROWS - 1) / ROWS;     // a thread's piece has one place in rows ROWS apart
   constexpr int OE = 16 / sizeof(TO), OP = 32 / OE, OROWS = kWave / OP, NO = 32 / OROWS;          // a wave stores OROWS rows of 32 columns at once
@@ -427,121 +445,113 @@ __global__ __launch_bounds__(kWave * WN * WM, PER) void k_gated_stream(GatedArgs
   const int64_t last = t + (tiles - 1 - t) / plan.row_groups * plan.row_groups;
   // What else a tile reads, a tile ahead: dh of the wave's rows (64 bytes or more side by side), scales of its 8-bit rows.
   constexpr int ND = 32 / OROWS;
-  Piece dhp[GRAD ? RB * ND : 1];
-  float scale[DEEP ? 1 : RB];
+  Piece dhp[GRAD ? ND : 1];
+  float scale = 1.f;
   auto fetch_more = [&](int64_t t, auto plain) {
+    const int64_t my_row = t * MR + wm * 32;
+    if constexpr (!DEEP) scale = a.x_scale[min(my_row + l % 32, a.rows - 1)];
+    if constexpr (GRAD)
 #pragma unroll
-    for (int rb = 0; rb < RB; rb++) {
-      const int64_t my_row = t * MR + (wm * RB + rb) * 32;
-      if constexpr (!DEEP) scale[rb] = a.x_scale[min(my_row + l % 32, a.rows - 1)];
-      if constexpr (GRAD)
-#pragma unroll
-        for (int j = 0; j < ND; j++) {
-          if constexpr (plain()) {
-            const char *base = reinterpret_cast<const char *>(static_cast<const TO *>(a.dh) + (my_row + j * OROWS) * a.ld_dh);
-            dhp[rb * ND + j] = (Piece)*reinterpret_cast<const PieceAny *>(base + d_at);
-          } else {
-            const int64_t r = min(my_row + j * OROWS + orow, a.rows - 1);
-            dhp[rb * ND + j] = (Piece)*reinterpret_cast<const PieceAny *>(static_cast<const TO *>(a.dh) + r * a.ld_dh + min(n0 + ocol, a.hidden - OE));
-          }
+      for (int j = 0; j < ND; j++) {
+        if constexpr (plain()) {
+          const char *base = reinterpret_cast<const char *>(static_cast<const TO *>(a.dh) + (my_row + j * OROWS) * a.ld_dh);
+          dhp[j] = (Piece)*reinterpret_cast<const PieceAny *>(base + d_at);
+        } else {
+          const int64_t r = min(my_row + j * OROWS + orow, a.rows - 1);
+          dhp[j] = (Piece)*reinterpret_cast<const PieceAny *>(static_cast<const TO *>(a.dh) + r * a.ld_dh + min(n0 + ocol, a.hidden - OE));
         }
-    }
+      }
   };
   // One tile.  PLAIN: not this workgroup's last one, and all 32 columns there: the stores are then under no condition, and the wait for the next
   // tile's rows is not one for them (one wave of a launch with a condition on its stores: 2.45M x 128 x 344 bf16 940 us).
   auto tile = [&](int64_t t, int buffer, auto plain) {
     constexpr bool PLAIN = plain();
     __syncthreads();
+    const int64_t my_row = t * MR + wm * 32;
+    f32x16 g = f32x16{}, u = f32x16{};
+    const char *xs = s_x + (buffer * MR + wm * 32) * P;
+    // fragments are asked for AHEAD steps before their products: left alone, the compiler asks for one at a time and waits for it
+    constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;
+    V f[AHEAD];
 #pragma unroll
-    for (int rb = 0; rb < RB; rb++) {
-      const int64_t my_row = t * MR + (wm * RB + rb) * 32;
-      f32x16 g = f32x16{}, u = f32x16{};
-      const char *xs = s_x + (buffer * MR + (wm * RB + rb) * 32) * P;
-      // fragments are asked for AHEAD steps before their products: left alone, the compiler asks for one at a time and waits for it
-      constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;
-      V f[AHEAD];
+    for (int s = 0; s < AHEAD; s++) f[s] = rows_frag<T>(xs, P, s);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int s = 0; s < AHEAD; s++) f[s] = rows_frag<T>(xs, P, s);
+    for (int s = 0; s < KS; s++) {
+      const V xf = f[s % AHEAD];
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          g = __builtin_amdgcn_mfma_f32_32x32x2f32(w[0][s][j], xf[j], g, 0, 0, 0);
+          u = __builtin_amdgcn_mfma_f32_32x32x2f32(w[1][s][j], xf[j], u, 0, 0, 0);
+        }
+      } else {
+        g = mma(w[0][s], xf, g);
+        u = mma(w[1][s], xf, u);
+      }
+      if (s + AHEAD < KS) f[s % AHEAD] = rows_frag<T>(xs, P, s + AHEAD);
       __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (GRAD) {
 #pragma unroll
-      for (int s = 0; s < KS; s++) {
-        const V xf = f[s % AHEAD];
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            g = __builtin_amdgcn_mfma_f32_32x32x2f32(w[0][s][j], xf[j], g, 0, 0, 0);
-            u = __builtin_amdgcn_mfma_f32_32x32x2f32(w[1][s][j], xf[j], u, 0, 0, 0);
-          }
-        } else {
-          g = mma(w[0][s], xf, g);
-          u = mma(w[1][s], xf, u);
-        }
-        if (s + AHEAD < KS) f[s % AHEAD] = rows_frag<T>(xs, P, s + AHEAD);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if constexpr (GRAD) {
-#pragma unroll
-        for (int j = 0; j < ND; j++) {
-          Piece &d = dhp[rb * ND + j];
-          if (!whole && n0 + ocol + OE > a.hidden) d = n0 + ocol < a.hidden ? move_down(d, n0 + ocol + OE - a.hidden, sizeof(TO)) : Piece{};
-          *reinterpret_cast<Piece *>(s_own + (orow + j * OROWS) * PO + l % OP * 16) = d;
-        }
-        wave_order();
-      }
-      constexpr int N = GRAD ? 8 : 16;         // elements at a time
-#pragma unroll
-      for (int q = 0; q < 16 / N; q++) {
-        float gv[N], uv[N];
-        TO *at = reinterpret_cast<TO *>(s_own + (l % 32) * PO) + 16 * q + 4 * half;          // four neighbouring columns at a time, 8 apart
-#pragma unroll
-        for (int e = 0; e < N; e++) {
-          gv[e] = g[8 * q + e];
-          uv[e] = u[8 * q + e];
-          if constexpr (!DEEP) {
-            gv[e] *= scale[rb] * s_scale[4 * q + 2 * (e / 4) + half][e % 4];
-            uv[e] *= scale[rb] * s_scale[8 + 4 * q + 2 * (e / 4) + half][e % 4];
-          }
-        }
-        if constexpr (GRAD) {
-          float dh[8];
-#pragma unroll
-          for (int e = 0; e < 2; e++) load_pack<TO, 4>(at + 8 * e, dh + 4 * e);
-          gate_grad_all<8>(gv, uv, dh, a.act);
-          if (!whole)                          // behind the last column the products that follow find zeros, whatever x holds
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-              if (n0 + 16 * q + 8 * (e / 4) + 4 * half + e % 4 >= a.hidden) gv[e] = uv[e] = 0.f;
-#pragma unroll
-          for (int e = 0; e < 2; e++) store_pack<TO, 4>(at + 32 * PO / (int)sizeof(TO) + 8 * e, uv + 4 * e);
-        } else gate_all<N>(gv, uv, a.act);
-#pragma unroll
-        for (int e = 0; e < N / 4; e++) store_pack<TO, 4>(at + 8 * e, gv + 4 * e);
-      }
-      if (rb == RB - 1) {
-        const int64_t next = min(t + plan.row_groups, last), after = min(t + 2 * plan.row_groups, last);
-        put(buffer ^ 1);
-        fetch(after);
-        // a last tile that is not full is asked for once more behind the loop, row by row; here this one stands in for it
-        fetch_more(!PLAIN || (next + 1) * MR <= a.rows ? next : t, plain);
-      }
-      wave_order();
-      char *base = reinterpret_cast<char *>(static_cast<TO *>(a.out) + my_row * a.ld_out + n0);
-      const char *mine = s_own + orow * PO + l % OP * 16;
-      const int64_t left = a.rows - my_row;
-#pragma unroll
-      for (int j = 0; j < (GRAD ? 2 : 1) * NO; j++) {
-        TO *to = reinterpret_cast<TO *>(base + ((int64_t)(j % NO) * OROWS * a.ld_out + j / NO * a.pad) * (int)sizeof(TO) + o_at);
-        const Piece v = *reinterpret_cast<const Piece *>(mine + j * OROWS * PO);
-        if constexpr (PLAIN) *reinterpret_cast<PieceAny *>(to) = v;
-        else {
-          if (orow + j % NO * OROWS >= left) continue;
-          if (GRAD || n0 + ocol + OE <= a.hidden) *reinterpret_cast<PieceAny *>(to) = v;
-          else
-            for (int e = 0; n0 + ocol + e < a.hidden; e++) to[e] = reinterpret_cast<const TO *>(mine + j * OROWS * PO)[e];
-        }
+      for (int j = 0; j < ND; j++) {
+        Piece &d = dhp[j];
+        if (!whole && n0 + ocol + OE > a.hidden) d = n0 + ocol < a.hidden ? move_down(d, n0 + ocol + OE - a.hidden, sizeof(TO)) : Piece{};
+        *reinterpret_cast<Piece *>(s_own + (orow + j * OROWS) * PO + l % OP * 16) = d;
       }
       wave_order();
     }
+    constexpr int N = GRAD || !DEEP ? 8 : 16;      // elements at a time: registers
+#pragma unroll
+    for (int q = 0; q < 16 / N; q++) {
+      float gv[N], uv[N];
+      TO *at = reinterpret_cast<TO *>(s_own + (l % 32) * PO) + 16 * q + 4 * half;          // four neighbouring columns at a time, 8 apart
+#pragma unroll
+      for (int e = 0; e < N; e++) {
+        gv[e] = g[8 * q + e];
+        uv[e] = u[8 * q + e];
+        if constexpr (!DEEP) {
+          gv[e] *= scale * s_scale[4 * q + 2 * (e / 4) + half][e % 4];
+          uv[e] *= scale * s_scale[8 + 4 * q + 2 * (e / 4) + half][e % 4];
+        }
+      }
+      if constexpr (GRAD) {
+        float dh[8];
+#pragma unroll
+        for (int e = 0; e < 2; e++) load_pack<TO, 4>(at + 8 * e, dh + 4 * e);
+        gate_grad_all<8>(gv, uv, dh, a.act);
+        if (!whole)                          // behind the last column the products that follow find zeros, whatever x holds
+#pragma unroll
+          for (int e = 0; e < 8; e++)
+            if (n0 + 16 * q + 8 * (e / 4) + 4 * half + e % 4 >= a.hidden) gv[e] = uv[e] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2; e++) store_pack<TO, 4>(at + 32 * PO / (int)sizeof(TO) + 8 * e, uv + 4 * e);
+      } else gate_all<N>(gv, uv, a.act);
+#pragma unroll
+      for (int e = 0; e < N / 4; e++) store_pack<TO, 4>(at + 8 * e, gv + 4 * e);
+    }
+    const int64_t next = min(t + plan.row_groups, last);
+    put(buffer ^ 1);
+    fetch(min(t + 2 * plan.row_groups, last));
+    // a last tile that is not full is asked for once more behind the loop, row by row; here this one stands in for it
+    fetch_more(!PLAIN || (next + 1) * MR <= a.rows ? next : t, plain);
+    wave_order();
+    char *base = reinterpret_cast<char *>(static_cast<TO *>(a.out) + my_row * a.ld_out + n0);
+    const char *mine = s_own + orow * PO + l % OP * 16;
+    const int64_t left = a.rows - my_row;
+#pragma unroll
+    for (int j = 0; j < (GRAD ? 2 : 1) * NO; j++) {
+      TO *to = reinterpret_cast<TO *>(base + ((int64_t)(j % NO) * OROWS * a.ld_out + j / NO * a.pad) * (int)sizeof(TO) + o_at);
+      const Piece v = *reinterpret_cast<const Piece *>(mine + j * OROWS * PO);
+      if constexpr (PLAIN) *reinterpret_cast<PieceAny *>(to) = v;
+      else {
+        if (orow + j % NO * OROWS >= left) continue;
+        if (GRAD || n0 + ocol + OE <= a.hidden) *reinterpret_cast<PieceAny *>(to) = v;
+        else
+          for (int e = 0; n0 + ocol + e < a.hidden; e++) to[e] = reinterpret_cast<const TO *>(mine + j * OROWS * PO)[e];
+      }
+    }
+    wave_order();
   };
   put(0);
   fetch(min(t + plan.row_groups, last));
@@ -708,8 +718,9 @@ __global__ __launch_bounds__(kWave * WM * WN, 2) void k_gated_dw(GatedDwArgs a) 
   constexpr int NX = KR * CX / THREADS, ND = KR * CD / THREADS, RX = THREADS / CX, RD = THREADS / CD;
   __shared__ __align__(16) char s_x[KR * PX], s_d[KR * PD];
   const int tid = threadIdx.x, l = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / kWave), wm = wave / WN, wn = wave % WN;
-  const int id = blockIdx.x / 8, tiles = a.tiles_c * a.tiles_n, slice = id / tiles * 8 + blockIdx.x % 8, tile = id % tiles;
-  if (slice >= a.slices) return;
+  const int tiles = a.tiles_c * a.tiles_n, id = blockIdx.x / 8;
+  const bool spread = a.slices % 8 != 0;     // few slices: over all chiplets
+  const int slice = spread ? blockIdx.x / tiles : id / tiles * 8 + blockIdx.x % 8, tile = spread ? blockIdx.x % tiles : id % tiles;
   const int c0 = tile % a.tiles_c * BM, n0 = tile / a.tiles_c * BN;
   const int64_t r_begin = slice * a.slice, r_end = min(r_begin + a.slice, a.rows);
   const int blocks = max(0, min(RI, (a.cols - c0 - wm * 32 * RI + 31) / 32)), wide = n0 + wn * 64 < 2 * a.pad;      // of x that there are; whether there are any of d
@@ -955,14 +966,16 @@ __global__ __launch_bounds__(kHeadThreads) void k_gated_dw_few(GatedFewArgs a) {
 }
 
 // ------------------------------------------------------------------------------------ host side
-// rows of x or of the weights that hold no whole piece of 16 bytes
-template <class T> static bool is_short(int cols, int hidden) { return std::min(cols, hidden) < 16 / (int)sizeof(T); }
 constexpr int64_t kFewRows = 16, kFewResults = 64 * 1024;    // as ink_linear: each workgroup asks for its columns of both matrices again for every row
 
-// Many rows, and a depth whose weights fit the registers: workgroups for the whole card, each with a stream of row tiles.
+// rows of x or of the weights that hold no whole piece of 16 bytes
+template <class T> static bool is_short(int cols, int hidden) { return std::min(cols, hidden) < 16 / (int)sizeof(T); }
+// Many rows, and a depth whose weights fit the registers: workgroups for the whole card, each with a stream of row tiles.  us a call, stream and tiles:
+// bf16 x 128 x 344 16384 rows 11.5 and 9.9, 32700 rows 14.9 and 16.5; x 256 x 683 8192 rows 17.5 and 16.2, 16384 rows 23 and 27; f32 x 128 x 344 16384
+// rows 38 and 37, 32700 rows 63 and 68.
 constexpr int64_t kStreamRows = 32 * 1024;
 template <class T, class TO, int KS, int WN, int WM, int PER, bool GRAD> static void stream_launch(const GatedArgs &a, Launches &run) {
-  constexpr int RB = stream_blocks<T, KS, WM>(), MR = 32 * RB * WM, P = KS * kTypeStep<T> * (int)sizeof(T) + 16, OWN = 32 * (32 * (int)sizeof(TO) + 16) * (GRAD ? 2 : 1), WAVES = WN * WM;
+  constexpr int MR = 32 * WM, P = KS * kTypeStep<T> * (int)sizeof(T) + 16, OWN = 32 * (32 * (int)sizeof(TO) + 16) * (GRAD ? 2 : 1), WAVES = WN * WM;
   constexpr int lds = 2 * MR * P + WAVES * (OWN + (sizeof(T) == 1 ? 256 : 0)), per_cu = std::max(1, std::min((160 << 10) / lds, 4 * PER / WAVES));
   static_assert(lds <= 160 << 10, "LDS holds two tiles of rows and the waves' results");
   const int wide = GRAD ? a.pad : a.hidden;
@@ -986,10 +999,11 @@ template <class T, class TO, int KS, int PER, bool GRAD> static void stream_wave
   stream_launch<T, TO, KS, 4, 1, PER, GRAD>(a, run);
 }
 template <class T, class TO, bool GRAD> static bool stream_run(const GatedArgs &a, Launches &run) {
-  if (a.rows < kStreamRows || a.cols < 16 / (int)sizeof(T) || a.hidden < 16 / (int)sizeof(TO) || (sizeof(T) > 1 && a.hidden < 16 / (int)sizeof(T))) return false;
+  const int steps = (a.cols + kTypeStep<T> - 1) / kTypeStep<T>;
+  if (a.rows < (sizeof(T) == 2 && steps > 8 ? kStreamRows / 2 : kStreamRows)) return false;
+  if (is_short<T>(a.cols, sizeof(T) == 1 ? a.cols : a.hidden) || a.hidden < 16 / (int)sizeof(TO)) return false;
   for (const int64_t ld : {a.ld_x, a.ld_out, a.ld_dh})
     if (ld >= 1 << 22) return false;         // offsets within a tile are 32-bit
-  const int steps = (a.cols + kTypeStep<T> - 1) / kTypeStep<T>;
   if constexpr (sizeof(T) == 4) {
     if (steps <= 8) stream_waves<T, TO, 8, 3, GRAD>(a, run);
     else if (steps <= 16) stream_waves<T, TO, 16, 2, GRAD>(a, run);
@@ -1000,7 +1014,7 @@ template <class T, class TO, bool GRAD> static bool stream_run(const GatedArgs &
     else return false;
   } else {
     if (steps <= 2) stream_waves<T, TO, 2, 3, GRAD>(a, run);
-    else if (steps <= 4) stream_waves<T, TO, 4, 2, GRAD>(a, run);
+    else if (steps <= 4) stream_waves<T, TO, 4, 3, GRAD>(a, run);
     else if (steps <= 8) stream_waves<T, TO, 8, 2, GRAD>(a, run);
     else return false;
   }
@@ -1050,12 +1064,20 @@ static GatedPlan gated_plan(int64_t rows, int cols, int hidden, int type) {
   p.wn = 4 / p.wm;
   p.tiles_c = (cols + 127) / 128;
   p.tiles_n = (2 * p.pad + 64 * p.wn - 1) / (64 * p.wn);
-  const int64_t steps = p.part_rows / 64, tiles = (int64_t)p.tiles_c * p.tiles_n;     // 64 rows: whole chunks of every type
-  const int64_t slices = std::max<int64_t>(1, std::min<int64_t>(steps / 2, (wide ? 512 : 1024) / tiles));
+  // Slices: eight (one a chiplet) times a number that leaves few of a chiplet's 64 or 96 places for workgroups empty (20k x 1024 x 4096
+  // in one slice 1586 us, in 8 579; 100k x 602 x 1605 in 7 808, in 16 664); fewer where the rows are few or
+  // the partial matrices would have more than 1 GB.
+  const int64_t steps = p.part_rows / 64, tiles = (int64_t)p.tiles_c * p.tiles_n, places = wide ? 64 : 96;          // 64 rows: whole chunks of every type
+  int64_t best = 1;
+  auto used = [&](int64_t k) { return (double)(k * tiles) / (double)((k * tiles + places - 1) / places * places); };
+  for (int64_t k = 2; k <= std::max<int64_t>(8, places / tiles) && k * tiles <= 4 * places; k++)
+    if (used(k) > used(best) + 0.02) best = k;
+  const int64_t tile_bytes = 128 * 64 * p.wn * 4;
+  const int64_t slices = std::max<int64_t>(1, std::min({steps / 2, 8 * best, (1ll << 30) / (tiles * tile_bytes)}));
   p.slice = (steps + slices - 1) / slices * 64;
-  p.slices = (int)((p.part_rows + p.slice - 1) / p.slice);
+  p.slices = (int)(slices >= 8 ? slices : (p.part_rows + p.slice - 1) / p.slice);
   p.d_bytes = p.part_rows * row_bytes;
-  p.part_bytes = (int64_t)p.slices * tiles * (128 * 64 * p.wn) * 4;
+  p.part_bytes = (int64_t)p.slices * tiles * tile_bytes;
   return p;
 }
 
@@ -1080,7 +1102,7 @@ template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void 
       GatedDwArgs q{b.x, work, reinterpret_cast<float *>(static_cast<char *>(work) + p.d_bytes), b.rows, a.ld_x, p.slice, a.cols, p.pad, r0 > 0, p.slices,
                     p.tiles_c, p.tiles_n};
       const auto kernel = p.ri == 4 ? (brief ? k_gated_dw<T, 4, 1, 4, true> : k_gated_dw<T, 4, 1, 4, false>) : (brief ? k_gated_dw<T, 2, 2, 2, true> : k_gated_dw<T, 2, 2, 2, false>);
-      run(kernel, dim3((unsigned)((p.slices + 7) / 8 * 8 * p.tiles_c * p.tiles_n)), dim3(256), q);
+      run(kernel, dim3((unsigned)(p.slices * p.tiles_c * p.tiles_n)), dim3(256), q);
     }
   }
 }

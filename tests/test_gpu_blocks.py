@@ -289,7 +289,7 @@ def test_gated_backward(rows, cols, hidden, dtype):
 # enough rows for the kernels that keep the weights in registers, or for their fallback (deep sums, few columns): every class of depth and
 # width, sizes beside the tiles', last tiles of one row, rows that no workgroup shares with another
 MANY = [(32768, 64, 32, 0), (32769, 128, 344, 3), (33000, 47, 31, 1), (32800, 100, 64, 2), (32769, 65, 172, 3), (32801, 8, 341, 0), (32790, 120, 130, 1),
-        (32777, 256, 100, 3), (33333, 250, 41, 2), (32769, 200, 300, 3), (32801, 7, 40, 1), (32769, 270, 50, 3), (32770, 33, 7, 2), (36000, 129, 8, 3)]
+        (32777, 256, 100, 3), (33333, 250, 41, 2), (32769, 200, 300, 3), (32801, 7, 40, 1), (32769, 270, 50, 3), (32770, 33, 7, 2), (36000, 129, 8, 3), (16385, 200, 70, 2)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
