@@ -1073,7 +1073,7 @@ static GatedPlan gated_plan(int64_t rows, int cols, int hidden, int type) {
   for (int64_t k = 2; k <= std::max<int64_t>(8, places / tiles) && k * tiles <= 4 * places; k++)
     if (used(k) > used(best) + 0.02) best = k;
   const int64_t tile_bytes = 128 * 64 * p.wn * 4;
-  const int64_t slices = std::max<int64_t>(1, std::min({steps / 2, 8 * best, (1ll << 30) / (tiles * tile_bytes)}));
+  const int64_t slices = std::max<int64_t>(1, std::min({steps / 2, 8 * best, (int64_t)(1 << 30) / (tiles * tile_bytes)}));
   p.slice = (steps + slices - 1) / slices * 64;
   p.slices = (int)(slices >= 8 ? slices : (p.part_rows + p.slice - 1) / p.slice);
   p.d_bytes = p.part_rows * row_bytes;
