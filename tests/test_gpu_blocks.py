@@ -359,3 +359,87 @@ def test_gated_of_no_rows_and_numbers_that_are_none():
         assert torch.equal(bad, ~torch.isfinite(x[rows].float()).all(1)), "other rows are untouched"
         dx = head.gated_backward(torch.ones(len(h), 5, device="cuda", dtype=BF16), x[rows].cuda(), w.to(BF16), w.to(BF16))[0]
         assert torch.equal(~torch.isfinite(dx.float().cpu()).all(1), bad)
+
+
+def test_more_rows_than_one_launch_takes():
+    """2^21 rows a launch in tiles (a depth that the registers do not hold), with scales of 8-bit rows beside them."""
+    rows, cols, hidden = 2 ** 21 + 100, 264, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(rows, cols, device="cuda", generator=g).to(BF16)
+    wg, wu = ((torch.randn(cols, hidden, device="cuda", generator=g) * cols ** -0.5).to(BF16) for _ in range(2))
+    h = head.gated(x, wg, wu)
+    some = torch.cat([torch.arange(0, 50), torch.arange(2 ** 21 - 50, rows)])
+    want, e = gated_ref(x[some.cuda()].double().cpu(), wg.double().cpu(), wu.double().cpu(), "silu", cols)
+    close(h[some.cuda()], want, e, BF16, "bf16")
+    x8, s8 = to_codes(x.float(), 1)
+    w8, sw = to_codes(wg.float().t(), 1)
+    h = head.gated(x8, w8.t(), w8.t(), x_scale=s8, gate_scale=sw, up_scale=sw, out_dtype=F32)
+    dx, dw = x8[some.cuda()].double().cpu() * s8[some.cuda()].double().cpu()[:, None], (w8.double() * sw.double()[:, None]).t().cpu()
+    want, e = gated_ref(dx, dw, dw, "silu", cols)
+    close(h[some.cuda()], want, e, F32, "e4m3")
+
+
+def test_gradient_of_several_parts():
+    """dg and du of 2 x 1024 columns: 262144 rows a part, three parts."""
+    rows, cols, hidden = 2 * 262144 + 77, 16, 1024
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, dh = torch.randn(rows, cols, device="cuda", generator=g).to(BF16), torch.randn(rows, hidden, device="cuda", generator=g).to(BF16)
+    wg, wu = ((torch.randn(cols, hidden, device="cuda", generator=g) * cols ** -0.5).to(BF16) for _ in range(2))
+    got = head.gated_backward(dh, x, wg, wu)
+    for a, (want, e), name in zip(got, gated_grad_ref(dh, x, wg, wu, "silu", BF16), ("dx", "dw_gate", "dw_up")):
+        close(a, want.cpu(), e.cpu(), BF16, name)
+    again = head.gated_backward(dh, x, wg, wu)
+    assert all(torch.equal(a, b) for a, b in zip(got, again)), "the same call gives the same bits"
+
+
+def test_another_stream_and_a_captured_call():
+    """The calls run on the current stream and can be captured; every replay gives what an eager call gives."""
+    g = gen(6)
+    x, res, dh = (torch.randn(n, 48, generator=g).to(BF16).cuda() for n in (700, 700, 700))
+    wg, wu = ((torch.randn(48, 48, generator=g) / 7).to(BF16).cuda() for _ in range(2))
+
+    def call():
+        y, total, rstd = head.rms_norm(x, wg[0], residual=res)
+        codes, scale, _, _ = head.rms_norm(x, wg[0], residual=res, out_dtype=E4M3)
+        h = head.gated(y, wg, wu)
+        dy, dg, du = head.gated_backward(dh, y, wg, wu)
+        return (h, dg, du, scale, codes.view(torch.uint8), *head.rms_norm_backward(dy, total, rstd, wg[0], d_total=dh))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        first = call()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for i in range(3):
+        x.copy_(torch.randn(700, 48, generator=g).to(BF16).cuda())
+        graph.replay()
+        torch.cuda.synchronize()
+        want = call()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+    assert not torch.equal(first[0], out[0])
+
+
+def test_refusals_of_the_binding():
+    x, w = torch.randn(4, 6, device="cuda"), torch.randn(6, 5, device="cuda")
+    e = x.to(E4M3)
+    w8 = w.to(E4M3)
+    one4, one5 = torch.ones(4, device="cuda"), torch.ones(5, device="cuda")
+    bad = [
+        (TypeError, lambda: head.rms_norm(x, out_dtype=BF16)), (TypeError, lambda: head.rms_norm(x.double())), (ValueError, lambda: head.rms_norm(x, residual=x[:3])),
+        (TypeError, lambda: head.rms_norm(x, residual=x.half())), (ValueError, lambda: head.rms_norm(x, one4)), (ValueError, lambda: head.rms_norm(x.clone().requires_grad_())),
+        (head.InkError, lambda: head.rms_norm(x, eps=0.0)), (ValueError, lambda: head.rms_norm_backward(x, x, None)), (ValueError, lambda: head.rms_norm_backward(x, x, one5)),
+        (ValueError, lambda: head.rms_norm_backward(x, x, one4, d_total=x[:, :5])), (TypeError, lambda: head.rms_norm_backward(x, x, one4, param_dtype=BF16)),
+        (ValueError, lambda: head.gated(x, w, w[:, :4])), (TypeError, lambda: head.gated(x, w.half(), w)), (ValueError, lambda: head.gated(x, w, w, act="tanh")),
+        (ValueError, lambda: head.gated(x, w, w, x_scale=one4)), (TypeError, lambda: head.gated(x, w, w, out_dtype=BF16)), (ValueError, lambda: head.gated(e, w8, w8)),
+        (TypeError, lambda: head.gated(e, w, w, x_scale=one4, gate_scale=one5, up_scale=one5)), (ValueError, lambda: head.gated(e, w8, w8, x_scale=one4, gate_scale=one4, up_scale=one5)),
+        (TypeError, lambda: head.gated(e, w8, w8, x_scale=one4, gate_scale=one5, up_scale=one5, out_dtype=E4M3)), (TypeError, lambda: head.gated_backward(e, e, w8, w8)),
+        (ValueError, lambda: head.gated_backward(x, x, w, w)), (TypeError, lambda: head.gated_backward(x[:, :5].half(), x, w, w)),
+    ]
+    for i, (kind, call) in enumerate(bad):
+        with pytest.raises(kind):
+            call()
+            print(i)
+    with torch.no_grad():
+        head.rms_norm(x.clone().requires_grad_())
