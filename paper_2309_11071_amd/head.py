@@ -8,10 +8,10 @@ gradient raises unless it is detached or the call stands under torch.no_grad(). 
 tensor whose rows are contiguous, at any distance from each other; any other layout is copied first.
 Tensors of other devices or types and shapes that do not fit raise.
 """
-import array
 import ctypes as C
 import itertools
 import operator
+import struct
 
 import torch
 
@@ -331,6 +331,8 @@ def _columns_8(w, name, cols, hidden, like):
         raise ValueError("%s must be a GPU tensor of shape [%d, %s] on the rows' device" % (name, cols, "hidden" if hidden is None else hidden))
     if w.dtype is not E4M3:
         raise TypeError("%s has type %s, wanted %s" % (name, w.dtype, E4M3))
+    if w.requires_grad:
+        _unrecorded(w, name)
     s0, s1 = w.stride()
     if (s0 != 1 and cols > 1) or (s1 < cols and s1 != 0 and w.shape[1] > 1):
         w = w.t().contiguous().t()
@@ -460,6 +462,7 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
         raise ValueError("moments must be adamw_moments', all of one width")
     sizes = list(map(_numel, p))
     at = _held(p, "a parameter", sizes, dev, _PARAMS)
+    types = list(map(_dtype, p))
     if any(map(_requires_grad, p)) and torch.is_grad_enabled() and not all(x.is_leaf for x in p):
         raise ValueError("a parameter that requires a gradient and is no leaf cannot be changed in place")
     if not set(map(_dtype, g)) <= TYPES.keys() or set(map(_device_index, g)) != {dev} or list(map(_shape, g)) != list(map(_shape, p)):
@@ -479,18 +482,21 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
     if copies is not None:
         copy = [copies[i] for i in place] if some else copies
         here = [i for i in range(n) if copy[i] is not None]
-        if any(p[i].dtype is not torch.float32 for i in here):
+        if any(types[i] is not torch.float32 for i in here):
             raise TypeError("a copy is of float32 parameters")
         if here:
             c = list(none)
             for i, x in zip(here, _held([copy[i] for i in here], "a copy", [sizes[i] for i in here], dev, _COPIES)):
                 c[i] = x
-    changed = [x for column in (at, *held, c) if column for x in column]
+    grad_at = list(map(_address, g))
+    changed = [*at, *itertools.chain.from_iterable(h for h in held if h), *(x for x in c if x)]
     if not all(sizes):                                                        # tensors without elements have no address of their own
-        changed = [x for column in (at, *held, c) if column for x, size in zip(column, sizes) if size]
-    changed = [x for x in changed if x] if len(here) < n else changed        # (no copy: 0)
-    if len(set(changed)) != len(changed):
+        changed = [x for column in (at, *held, c) if column for x, size in zip(column, sizes) if x and size]
+    once = set(changed)
+    if len(once) != len(changed):
         raise ValueError("a tensor that the step changes stands in the call twice")
+    if not once.isdisjoint(grad_at if all(sizes) else [x for x, size in zip(grad_at, sizes) if size]):
+        raise ValueError("a gradient stands in the memory of a tensor that the step changes")
     step_at = scale_at = None
     if isinstance(step, torch.Tensor):
         if step.dtype is not torch.int64 or step.numel() != 1 or step.get_device() != dev:
@@ -503,14 +509,19 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
             _unrecorded(grad_scale, "grad_scale")
         scale_at, grad_scale = grad_scale.data_ptr(), 1.0
     lib = _functions()
-    entries = list(zip(at, map(_address, g), c, held[0], held[2], held[1] or none, held[3] or none, sizes, place))
-    kinds = list(zip(map(_dtype, p), map(_dtype, g), [None if x is None else x.dtype for x in copy] if here else none))
-    for kind in dict.fromkeys(kinds):
-        mine = [e for e, k in zip(entries, kinds) if k == kind]
-        table = array.array("q", itertools.chain.from_iterable(mine))
-        tp, tg, tc = kind
-        _call(lib.ink_adamw, like, table.buffer_info()[0], len(mine), TYPES[tp], TYPES[tg], TYPES[tc] if tc else -1, 8 if width == 4 else 32, lr, betas[0], betas[1],
-              eps, weight_decay, step, step_at, grad_scale, scale_at, seed & 0xFFFFFFFFFFFFFFFF)
+    columns = at, grad_at, c, held[0], held[2], held[1] or none, held[3] or none, sizes, place
+    kinds = types, list(map(_dtype, g)), [None if x is None else x.dtype for x in copy] if here else none
+    groups = {}
+    if all(k.count(k[0]) == n for k in kinds):
+        groups[tuple(k[0] for k in kinds)] = zip(*columns)
+    else:
+        for kind, entry in zip(zip(*kinds), zip(*columns)):
+            groups.setdefault(kind, []).append(entry)
+    for (tp, tg, tc), entries in groups.items():
+        numbers = list(itertools.chain.from_iterable(entries))
+        table = struct.pack("%dq" % len(numbers), *numbers)
+        _call(lib.ink_adamw, like, table, len(numbers) // len(columns), TYPES[tp], TYPES[tg], TYPES[tc] if tc else -1, 8 if width == 4 else 32, lr, betas[0],
+              betas[1], eps, weight_decay, step, step_at, grad_scale, scale_at, seed & 0xFFFFFFFFFFFFFFFF)
     # what autograd has kept of these tensors is no longer what they hold
     torch.autograd.graph.increment_version(p)
     if here:

@@ -331,6 +331,42 @@ def test_refusals():
     refused(ValueError, [q * 1], [torch.ones(4, device="cuda")], head.adamw_moments([q]), 1)
 
 
+def test_a_gradient_that_the_step_changes_is_refused():
+    """A gradient in the memory of a parameter, a moment or a copy would be read while it changes."""
+    p = [torch.zeros(300, device="cuda") for _ in range(2)]
+    g = [torch.ones(300, device="cuda") for _ in range(2)]
+    mom, copies = head.adamw_moments(p), [x.to(BF16) for x in p]
+    for bad in ([p[1], g[1]], [g[0], mom[0][1]], [mom[1][0], g[1]], [g[0], copies[0]]):
+        with pytest.raises((ValueError, TypeError)):
+            head.adamw(p, bad, mom, 1, copies=copies)
+    assert not any(x.any() for x in p + copies + [m for e in mom for m in e]), "nothing was changed"
+    empty = [torch.zeros(0, device="cuda"), p[0]]
+    head.adamw(empty, [torch.zeros(0, device="cuda"), g[0]], head.adamw_moments(empty), 1, lr=0.5, weight_decay=0.0)
+    assert torch.allclose(p[0], torch.full((300,), -0.5, device="cuda"))
+    head.adamw(p, [g[0], g[0]], mom, 1, lr=0.5, weight_decay=0.0)            # one gradient for two parameters is read only
+    assert torch.allclose(p[1], torch.full((300,), -0.5, device="cuda"))
+
+
+def test_types_that_differ_within_a_list():
+    """Tensors of several types, some with a copy: every one gets the step of a call by itself."""
+    rand = torch.Generator().manual_seed(31)
+    kinds = [(F32, BF16, BF16), (F32, F32, None), (BF16, BF16, None), (F32, BF16, torch.float16), (F32, BF16, BF16)]
+    start = [torch.randn(1000 + i, generator=rand).cuda().to(k[0]) for i, k in enumerate(kinds)]
+    g = [torch.randn(1000 + i, generator=rand).cuda().to(k[1]) for i, k in enumerate(kinds)]
+
+    def state():
+        p = [x.clone() for x in start]
+        return p, head.adamw_moments(p, 8), [None if k[2] is None else torch.zeros(x.shape, dtype=k[2], device="cuda") for x, k in zip(p, kinds)]
+    p, mom, copies = state()
+    head.adamw(p, g, mom, 1, copies=copies, seed=5)
+    for i in range(len(kinds)):
+        q, one, c = state()
+        head.adamw(q, [x if j == i else None for j, x in enumerate(g)], one, 1, copies=c, seed=5)
+        assert torch.equal(q[i], p[i]) and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(one[i], mom[i]))
+        assert copies[i] is None or torch.equal(c[i], copies[i])
+        assert all(torch.equal(q[j], start[j]) for j in range(len(kinds)) if j != i)
+
+
 def test_autograd_sees_the_change():
     """What autograd keeps of a parameter for a backward pass is out of date after the step; a leaf that requires a gradient is an ordinary parameter."""
     q, x = torch.ones(4, device="cuda", requires_grad=True), torch.ones(4, device="cuda", requires_grad=True)

@@ -443,3 +443,14 @@ def test_refusals_of_the_binding():
             print(i)
     with torch.no_grad():
         head.rms_norm(x.clone().requires_grad_())
+
+
+def test_8_bit_weights_that_require_a_gradient_raise():
+    """As every tensor of these calls: nothing records the call for autograd."""
+    x, w, s = torch.zeros(2, 16, device="cuda").to(E4M3), torch.zeros(8, 16, device="cuda").to(E4M3).t(), torch.ones(8, device="cuda")
+    wanted = w.detach().requires_grad_()
+    for gate, up in ((wanted, w), (w, wanted)):
+        with pytest.raises(ValueError):
+            head.gated(x, gate, up, x_scale=s[:2], gate_scale=s, up_scale=s)
+        with torch.no_grad():
+            assert not head.gated(x, gate, up, x_scale=s[:2], gate_scale=s, up_scale=s).any()
