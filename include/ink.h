@@ -78,8 +78,8 @@ typedef enum {
   INK_AGG_MAX = 0, INK_AGG_MIN = 1, INK_AGG_SUM = 2, INK_AGG_MEAN = 3, INK_AGG_GCN_SYM = 4
 } ink_agg;
 
-/* GELU (z times the normal distribution function) and SILU (z times the logistic function): ink_linear only,
- * a layer takes NONE or RELU. */
+/* GELU (z times the normal distribution function) and SILU (z times the logistic function): ink_linear and
+ * ink_gated only, a layer takes NONE or RELU. */
 typedef enum { INK_ACT_NONE = 0, INK_ACT_RELU = 1, INK_ACT_GELU = 2, INK_ACT_SILU = 3 } ink_act;
 typedef enum { INK_F32 = 0, INK_BF16 = 1, INK_F16 = 2, /* element types of an answer head's operators */
                INK_E4M3 = 3, /* 8 bits (4 of exponent, 3 of mantissa, largest number 448), where an operator says so */
@@ -351,8 +351,8 @@ ink_status ink_get_stats(ink_ctx *ctx, void *stats_out, size_t bytes);
 
 /* ---------------------------------------------------------------- operators of an answer head
  *
- * What turns embeddings into answers, and re-fits that map while the graph changes: layer norm, a
- * linear layer with its epilogue, log probabilities of classes; each with its gradient.  They need no context
+ * What turns embeddings into answers, and re-fits that map while the graph changes: layer norm, root-mean-square norm, a
+ * linear layer with its epilogue, a gated pair of projections, log probabilities of classes; each with its gradient; and a step of AdamW.  They need no context
  * and take rows from anywhere on the device, an update's result (ink_update_result) among them.
  *
  * Unlike the calls on a context these are ASYNCHRONOUS: a call enqueues its kernels on `hip_stream`
@@ -461,7 +461,7 @@ ink_status ink_rms_norm_backward(const void *dy, int64_t ld_dy, const void *tota
  *   act          ink_act
  * Of 8-bit rows (type INK_E4M3, ink_rms_norm's): row r of x is x_scale[r] times its numbers; the weights lie column by column,
  * [hidden][cols], and column c of Wg is gate_scale[c] times its numbers, of Wu up_scale[c] times; out_type is any of the other three.  The
- * scales are float and not read for other types. */
+ * scales are float and not read for other types; x_scale[r] * gate_scale[c] is formed in 32 bits and should be a normal number. */
 ink_status ink_gated(const void *x, int64_t ld_x, const float *x_scale, const void *w_gate, int64_t ld_gate, const void *w_up,
                      int64_t ld_up, const float *gate_scale, const float *up_scale, int64_t rows, int32_t cols, int32_t hidden, int32_t type,
                      int32_t out_type, int32_t act, void *h, int64_t ld_h, void *hip_stream);
@@ -484,10 +484,12 @@ ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int6
  *   moment_bits  32: m and v are float arrays.  8: m and v are INK_E4M3 arrays, and of each INK_ADAMW_BLOCK neighbouring elements m is
  *                m_scale times the number of its code, sqrt(v) v_scale times that of its code; zeros everywhere are the moments at the start
  *   step         t, from 1; or step_at, one int64 on the device that holds it (a captured call reads it at every replay; below 1 counts as 1)
- *   seed         of the random numbers that round 8-bit moments and INK_BF16 parameters: up or down, in proportion (unbiased).  The
- *                numbers depend on seed, t, the tensor's id and the element, and on nothing else
- *   lr and weight_decay >= 0;  betas in [0, 1);  eps > 0
- * A gradient that is NaN or infinite makes its element NaN, with 8-bit moments the moments of its block. */
+ *   seed         of the random numbers that round 8-bit moments and INK_BF16 parameters: up or down, in proportion, so that the expectation of
+ *                a parameter, of m and of sqrt(v) is what was to be rounded (that of v is larger by the variance).  The numbers depend on
+ *                seed, t, the tensor's id and the element, and on nothing else
+ *   lr and weight_decay 0 .. 1e18;  betas in [0, 1);  eps > 0
+ * A gradient that is NaN or infinite makes its element NaN, with 8-bit moments the moments of its block; so does, with 8-bit moments, one
+ * whose square is beyond a float (with 32-bit ones its element stays where it is, but for the decay). */
 typedef struct {
   void *param;
   const void *grad;

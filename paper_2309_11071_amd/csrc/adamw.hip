@@ -230,10 +230,10 @@ extern "C" ink_status ink_adamw(const ink_adamw_tensor *tensors, int32_t n_tenso
   if (!known_type(grad_type)) return refuse("unknown type of the gradients");
   if (copy_type != INK_NO_TYPE && ((copy_type != INK_BF16 && copy_type != INK_F16) || param_type != INK_F32)) return refuse("a copy is INK_BF16 or INK_F16, of INK_F32 parameters");
   if (moment_bits != 32 && moment_bits != 8) return refuse("moments have 32 or 8 bits");
-  if (!(lr >= 0 && lr < 1e30)) return refuse("lr must be finite and not negative");
+  if (!(lr >= 0 && lr <= 1e18)) return refuse("lr must be 0 .. 1e18");        // its product with 1 / (1 - beta1), or with the decay, is a float
   if (!(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1)) return refuse("the betas must lie in [0, 1)");
   if (!(eps >= 1.2e-38 && eps < 1e30)) return refuse("eps must be positive, a normal float and finite");
-  if (!(weight_decay >= 0 && weight_decay < 1e30)) return refuse("weight_decay must be finite and not negative");
+  if (!(weight_decay >= 0 && weight_decay <= 1e18)) return refuse("weight_decay must be 0 .. 1e18");
   if (!(std::fabs(grad_scale) < 3e38)) return refuse("grad_scale must be finite");
   if (!step_at && step < 1) return refuse("steps count from 1");
   if (!aligned_to(step_at, 8) || !aligned_to(grad_scale_at, 4)) return refuse("step_at or grad_scale_at is not aligned");

@@ -167,15 +167,15 @@ template <int N> __device__ __forceinline__ void gate_grad_all(float g[N], float
 }
 
 // ------------------------------------------------------------------------------------ tiles
-// 64 RB rows by 64 columns of h a workgroup, 32 RB by 32 a wave (a tile of Wg and one of Wu, so that g and u of an element meet in a lane), 128 bytes
+// 128 rows by 64 columns of h a workgroup, 64 by 32 a wave (a tile of Wg and one of Wu, so that g and u of an element meet in a lane), 128 bytes
 // of the depth at a time: while one piece is multiplied the next is on its way in registers.  16-bit weights lie in LDS as they do in memory, and the
 // transposing read makes fragments of their columns.  100k x 602 x 1605 bf16 700 us (550 TFLOP/s), which LDS bounds: a wave reads 4 KB of it for four
 // products of 32 cycles.
 // TL: type of the operands in memory, T: in the products, TO: of h.  GRAD: dg and du go to `out` in place of h.
-template <class TL, class T, class TO, int RB, bool GRAD, bool SHORT>
+template <class TL, class T, class TO, bool GRAD, bool SHORT>
 __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
   typedef typename Frag<T>::V V;
-  constexpr int BM = 64 * RB, KC = kChunkK<T>, PE = 16 / sizeof(T), STEPS = KC / kTypeStep<T>;
+  constexpr int RB = 2, BM = 64 * RB, KC = kChunkK<T>, PE = 16 / sizeof(T), STEPS = KC / kTypeStep<T>;
   constexpr bool DEEP = sizeof(TL) != 1;     // the depth runs down the weights' columns
   constexpr int PW = DEEP ? 2 * kTileHidden * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 16) : kChunkPitch;
   constexpr int NX = BM * 8 / 256, NW = 4;
@@ -989,7 +989,8 @@ template <class T, class TO, int KS, int WN, int WM, int PER, bool GRAD> static 
 }
 // Four waves a workgroup, one on every SIMD of its CU (workgroups of six leave no room for a second one although its registers are there), or, where the
 // columns fill them about as well, twelve, three on every SIMD: rows of results then leave a workgroup whole, which counts where they are no multiple of
-// whole lines (2.45M x 128 x 341 bf16 722 us with twelve waves, 872 with three workgroups of four; x 344 660 and 765; x 384 654 and 692).
+// whole lines (2.45M x 128 x 341 bf16 722 us with twelve waves, 872 with three workgroups of four; x 344 660 and 765; x 384 654 and 692).  With one or two
+// waves side by side a thread has more of the rows under way and some registers spill, as in linear.hip; their calls wait for the rows.
 template <class T, class TO, int KS, int PER, bool GRAD> static void stream_waves(const GatedArgs &a, Launches &run) {
   const int tiles = ((GRAD ? a.pad : a.hidden) + 31) / 32;
   if (tiles == 1) return stream_launch<T, TO, KS, 1, sizeof(T) == 4 ? 2 : 4, PER, GRAD>(a, run);
@@ -1031,7 +1032,7 @@ template <class TL, class T, class TO> static void gated_tiles(const GatedArgs &
     b.out = static_cast<TO *>(a.out) + r0 * a.ld_out;
     if (a.x_scale) b.x_scale = a.x_scale + r0;
     const int64_t tiles = (b.rows + 127) / 128;
-    run(is_short<T>(a.cols, a.hidden) ? k_gated_tile<TL, T, TO, 2, false, true> : k_gated_tile<TL, T, TO, 2, false, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * gy)), dim3(256), b);
+    run(is_short<T>(a.cols, a.hidden) ? k_gated_tile<TL, T, TO, false, true> : k_gated_tile<TL, T, TO, false, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * gy)), dim3(256), b);
   }
 }
 template <class T, class TO> static void gated_run(const GatedArgs &a, Launches &run) {
@@ -1091,7 +1092,7 @@ template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void 
     b.x = static_cast<const T *>(a.x) + r0 * a.ld_x;
     b.dh = static_cast<const T *>(a.dh) + r0 * a.ld_dh;
     const int64_t tiles = (b.rows + 127) / 128;
-    if (!stream_run<T, T, true>(b, run)) run(brief ? k_gated_tile<T, T, T, 2, true, true> : k_gated_tile<T, T, T, 2, true, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * ((a.hidden + kTileHidden - 1) / kTileHidden))), dim3(256), b);
+    if (!stream_run<T, T, true>(b, run)) run(brief ? k_gated_tile<T, T, T, true, true> : k_gated_tile<T, T, T, true, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * ((a.hidden + kTileHidden - 1) / kTileHidden))), dim3(256), b);
     if (dx) {
       GatedDxArgs q{work, a.gate, a.up, static_cast<T *>(dx) + r0 * ld_dx, b.rows, a.ld_gate, a.ld_up, ld_dx, a.cols, a.hidden, p.pad};
       const int gy = (a.cols + 127) / 128;

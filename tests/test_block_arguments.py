@@ -94,6 +94,12 @@ def test_bad_arguments_are_refused(lib, i):
     assert lib.ink_last_error(None).decode().startswith(NAMES[call])
 
 
+def test_rates_that_pass_a_floats_range_are_refused(lib):
+    """lr / (1 - beta1) and lr times the decay are floats on the device: their factors end at 1e18."""
+    assert adamw(lib, lr=1.1e18) == E_ARG and adamw(lib, wd=1.1e18) == E_ARG
+    assert adamw(lib, n=0, lr=1e18, wd=1e18) == 0
+
+
 def test_no_rows_need_no_memory(lib):
     assert rms(lib, x=None, res=None, y=None, total=None, rstd=None, rows=0) == 0
     assert rms(lib, x=None, res=M, y=None, total=None, rstd=None, rows=0, out=3) == 0
