@@ -468,8 +468,9 @@ ink_status ink_gated(const void *x, int64_t ld_x, const float *x_scale, const vo
 
 /* Gradient of ink_gated (not of 8-bit rows), with g = x Wg and u = x Wu formed anew: dg = dh u act'(g), du = dh act(g), dx = dg Wg^T + du Wu^T
  * [rows][cols], dw_gate = x^T dg and dw_up = x^T du [cols][hidden], all of `type`; each may be NULL (not wanted).  With 16-bit rows
- * dg and du are rounded to `type` before the products, but for a few rows.  The work memory does not grow with the rows beyond 2 GB, or
- * 1 GB and a matrix of [cols][2 hidden] floats where that has more. */
+ * dg and du are rounded to `type` before the products, but for a few rows; those of float16 rows with powers of two beside them, so that they may lie
+ * beyond float16's range where the results do not.  The work memory does not grow with the rows beyond 2.1 GB, or
+ * 1.1 GB and a matrix of [cols][2 hidden] floats where that has more. */
 size_t ink_gated_backward_work(int64_t rows, int32_t cols, int32_t hidden, int32_t type);
 ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int64_t ld_x, const void *w_gate, int64_t ld_gate,
                               const void *w_up, int64_t ld_up, int64_t rows, int32_t cols, int32_t hidden, int32_t type, int32_t act, void *dx,

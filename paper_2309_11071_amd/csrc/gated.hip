@@ -17,7 +17,7 @@
 // The gradient does not keep g and u: forming them again costs 4 rows cols hidden operations, keeping them 8 bytes an element of h written and
 // read (1M x 128 x 344 bf16: 0.16 ms of the matrix unit against 0.55 ms of memory).  dg and du are left in work memory once, in the rows' type, for the two
 // products that read them: an error of the size of the results' own rounding (233k x 256 x 683 bf16 0.0024 from 64 bits where rounding the results alone
-// gives 0.0017).  A few rows are kept in 32 bits.  The weights' gradients are sums over all rows: workgroups take slices of the rows and leave a
+// gives 0.0017).  float16 rows keep their range besides (GatedRange).  A few rows are kept in 32 bits.  The weights' gradients are sums over all rows: workgroups take slices of the rows and leave a
 // partial matrix each, added up in order (no atomics: the same call gives the same bits).
 #include <algorithm>
 #include <type_traits>
@@ -81,12 +81,68 @@ template <class TL, class T, bool SHORT> __device__ __forceinline__ Piece piece_
   } else return v;
 }
 
+// The range of dg and du of float16 rows: both may pass 65504, or lie below 2^-24 where many of them or a large weight make a result of them.
+// So 32 rows by 32 columns of them, a block, are held in units of 2^K.  K is 0 while the block's largest number lies between 2^-4 and 65504, and every number is
+// then what its rounding gives; else a multiple of 4 or 16, so that neighbouring blocks mostly agree.  A row of the block whose largest number would fall below 2^-12 there, and any
+// row of up to 65504 in a block beyond it, has units 2^-d times as large, so that a row beside one of quite another size keeps its own numbers: dx is formed
+// row by row.  For the sums over rows all are brought to the block's units.  The sums of products change their units, by a power of two, where the next block has others.
+// What it costs: 233k x 256 x 683 906 -> 944 us, 1M x 128 x 344 1297 -> 1412 us, most of it in the forming of dg and du; with sizes that differ from row to row by up to
+// 2^23 1230 and 1814 us.
+struct GatedRange {
+  int32_t *unit;                             // [row blocks][across]: 2 K, and 1 more where a row has units of its own
+  uint8_t *finer;                            // [row blocks][across][32]: d of the block's rows, written where that is so
+  int across;                                // blocks side by side: dg's, then du's
+};
+template <class T> constexpr bool kRanged = std::is_same_v<T, f16>;
+
+__device__ __forceinline__ int exponent_of(float a) { return (int)(__float_as_uint(a) >> 23) - 127; }            // of a >= 0
+__device__ __forceinline__ int unit_for(float top) {
+  const int e = exponent_of(top);
+  return top > 65504.f ? (e - 10) / 4 * 4 : top > 0.f && e < -4 ? -((11 - e) / 16 * 16) : 0;
+}
+// Brings 16 numbers a lane, lanes l and l ^ 32 a row's 32, a wave a block's, to their units, and writes these down.  Infinities and NaN stay and do not count.
+__device__ __forceinline__ void to_units(float v[16], const GatedRange &range, int64_t row_block, int column_block) {
+  const int64_t block = row_block * range.across + column_block;
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 16; j++) top = fmaxf(top, fabsf(v[j]));                   // the larger of a NaN and a number is the number
+  // Units of 1 for all, as a rule: seen by comparisons alone (with the reductions below for every block 233k x 256 x 683 973 us instead of 944)
+  int code = 0;
+  const bool ordinary = __builtin_amdgcn_ballot_w64(top >= 0.000244140625f || top == 0.f) == ~0ull;
+  if (!ordinary || __builtin_amdgcn_ballot_w64(top > 65504.f) || !__builtin_amdgcn_ballot_w64(top >= 0.0625f)) {
+    if (__builtin_amdgcn_ballot_w64(top == INFINITY)) {
+      top = 0.f;
+#pragma unroll
+      for (int j = 0; j < 16; j++) top = fmaxf(top, fabsf(v[j]) <= 3.4028235e38f ? fabsf(v[j]) : 0.f);
+    }
+    const auto larger = [](float a, float b) { return fmaxf(a, b); };
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const int unit = __builtin_amdgcn_readfirstlane(unit_for(group_all<32>(top, larger)));
+    const int calm = min(unit, 0), finer = unit - (top > 65504.f || (top > 0.f && exponent_of(top) - calm < -12) ? unit_for(top) : calm);
+    const bool uneven = __builtin_amdgcn_ballot_w64(finer != 0) != 0;
+#pragma unroll
+    for (int j = 0; j < 16; j++) v[j] = __builtin_amdgcn_ldexpf(v[j], finer - unit);
+    if (uneven) range.finer[block * 32 + lane_id() % 32] = (uint8_t)finer;
+    code = 2 * unit + uneven;
+  }
+  range.unit[block] = code;                  // by all lanes: a store under a condition would make the next wait for rows one for all stores
+}
+// A product's sums so far from units of 2^was to those of 2^unit
+template <int N> __device__ __forceinline__ void change_units(f32x16 (&acc)[N], int was, int unit) {
+#pragma unroll
+  for (int n = 0; n < N; n++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) acc[n][e] = __builtin_amdgcn_ldexpf(acc[n][e], was - unit);
+}
+
 struct GatedArgs {
   const void *x, *gate, *up, *dh;
   const float *x_scale, *gate_scale, *up_scale;
   void *out;                                 // forward: h; gradient: [rows][2 pad] of dg and du
   int64_t rows, ld_x, ld_gate, ld_up, ld_dh, ld_out;
   int cols, hidden, act, pad;                // pad: hidden rounded up to 32
+  GatedRange range;                          // gradient, float16
 };
 
 constexpr int kChunk = 128, kChunkPitch = kChunk + 16;     // bytes of the depth in LDS at a time, and between rows there
@@ -302,6 +358,11 @@ __global__ __launch_bounds__(256, 2) void k_gated_tile(GatedArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; e++)
           if (n0 + wn * 32 + 8 * (e / 4) + 4 * half + e % 4 >= a.hidden) gv[e] = uv[e] = 0.f;
+      if constexpr (kRanged<TO>)
+        if (n0 + wn * 32 < a.pad) {
+          to_units(gv, a.range, m0 / 32 + wm * RB + i, n0 / 32 + wn);
+          to_units(uv, a.range, m0 / 32 + wm * RB + i, (a.pad + n0) / 32 + wn);
+        }
 #pragma unroll
       for (int e = 0; e < 4; e++) store_pack<TO, 4>(at + BM * PO / (int)sizeof(TO) + 8 * e, uv + 4 * e);
     } else gate_all<16>(gv, uv, a.act);
@@ -502,9 +563,11 @@ __global__ __launch_bounds__(kWave * WN * WM, PER) void k_gated_stream(GatedArgs
       wave_order();
     }
     constexpr int N = GRAD || !DEEP ? 8 : 16;      // elements at a time: registers
+    constexpr bool WHOLE = GRAD && kRanged<TO>;    // stored when all are there: a block's units follow from all of it
+    float all_g[WHOLE ? 16 : N], all_u[WHOLE ? 16 : N];
 #pragma unroll
     for (int q = 0; q < 16 / N; q++) {
-      float gv[N], uv[N];
+      float *gv = all_g + (WHOLE ? N * q : 0), *uv = all_u + (WHOLE ? N * q : 0);
       TO *at = reinterpret_cast<TO *>(s_own + (l % 32) * PO) + 16 * q + 4 * half;          // four neighbouring columns at a time, 8 apart
 #pragma unroll
       for (int e = 0; e < N; e++) {
@@ -524,11 +587,23 @@ __global__ __launch_bounds__(kWave * WN * WM, PER) void k_gated_stream(GatedArgs
 #pragma unroll
           for (int e = 0; e < 8; e++)
             if (n0 + 16 * q + 8 * (e / 4) + 4 * half + e % 4 >= a.hidden) gv[e] = uv[e] = 0.f;
+        if constexpr (!WHOLE)
 #pragma unroll
-        for (int e = 0; e < 2; e++) store_pack<TO, 4>(at + 32 * PO / (int)sizeof(TO) + 8 * e, uv + 4 * e);
+          for (int e = 0; e < 2; e++) store_pack<TO, 4>(at + 32 * PO / (int)sizeof(TO) + 8 * e, uv + 4 * e);
       } else gate_all<N>(gv, uv, a.act);
+      if constexpr (!WHOLE)
 #pragma unroll
-      for (int e = 0; e < N / 4; e++) store_pack<TO, 4>(at + 8 * e, gv + 4 * e);
+        for (int e = 0; e < N / 4; e++) store_pack<TO, 4>(at + 8 * e, gv + 4 * e);
+    }
+    if constexpr (WHOLE) {
+      to_units(all_g, a.range, my_row / 32, n0 / 32);
+      to_units(all_u, a.range, my_row / 32, (a.pad + n0) / 32);
+      TO *at = reinterpret_cast<TO *>(s_own + (l % 32) * PO) + 4 * half;
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        store_pack<TO, 4>(at + 8 * e, all_g + 4 * e);
+        store_pack<TO, 4>(at + 32 * PO / (int)sizeof(TO) + 8 * e, all_u + 4 * e);
+      }
     }
     const int64_t next = min(t + plan.row_groups, last);
     put(buffer ^ 1);
@@ -581,6 +656,7 @@ struct GatedDxArgs {
   void *dx;
   int64_t rows, ld_gate, ld_up, ld_dx;
   int cols, hidden, pad;
+  GatedRange range;
 };
 template <class T, bool SHORT>
 __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedDxArgs a) {
@@ -596,6 +672,15 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedDxArgs a) {
   const int n0 = id % gy * BN;
   if (m0 >= a.rows) return;
   Piece d[ND], w[NW];
+  constexpr bool RANGED = kRanged<T>;
+  int unit[RI][2], next_unit[RI][2], was[RI], was_code[RI];            // of a lane's row, and as the blocks have them
+  int64_t blocks[RI];
+  if constexpr (RANGED)
+#pragma unroll
+    for (int i = 0; i < RI; i++) {
+      blocks[i] = min(m0 / 32 + wm * RI + i, (a.rows - 1) / 32) * a.range.across;
+      was[i] = was_code[i] = 0;
+    }
   const int at = tid % 8 * PE, row = tid / 8;
   const T *dp = static_cast<const T *>(a.d) + m0 * 2 * a.pad + at;
   uint32_t d_row[ND];
@@ -610,6 +695,11 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedDxArgs a) {
     const int64_t ld = second ? a.ld_up : a.ld_gate;
 #pragma unroll
     for (int j = 0; j < NW; j++) w[j] = raw_piece<T, T, SHORT>(from + (int64_t)min(n0 + row + RS * j, a.cols - 1) * ld, k, a.hidden);
+    if constexpr (RANGED)
+#pragma unroll
+      for (int i = 0; i < RI; i++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) next_unit[i][h] = a.range.unit[blocks[i] + k0 / 32 + h];
   };
   auto put = [&](int k0) {
     const int k = k0 + at - (k0 + at >= a.pad ? a.pad : 0);
@@ -626,10 +716,25 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedDxArgs a) {
   __syncthreads();
   for (int k0 = 0; k0 < 2 * a.pad; k0 += KC) {
     const bool more = k0 + KC < 2 * a.pad;
+    if constexpr (RANGED)
+#pragma unroll
+      for (int i = 0; i < RI; i++) { unit[i][0] = next_unit[i][0]; unit[i][1] = next_unit[i][1]; }
     if (more) fetch(k0 + KC);
 #pragma unroll
     for (int s = 0; s < 4; s++) {
       V ds[RI], ws[2];
+      if constexpr (RANGED)
+        if (s % 2 == 0)                        // 32 columns of d: a block
+#pragma unroll
+          for (int i = 0; i < RI; i++) {
+            const int code = unit[i][s / 2];
+            if (code == was_code[i] && !(code & 1)) continue;
+            int now = code >> 1;
+            if (code & 1) now -= a.range.finer[(blocks[i] + k0 / 32 + s / 2) * 32 + l % 32];
+            change_units(acc[i], was[i], now);
+            was[i] = now;
+            was_code[i] = code;
+          }
 #pragma unroll
       for (int n = 0; n < 2; n++) ws[n] = rows_frag<T>(s_w + (wn * 2 + n) * 32 * P, P, s);
 #pragma unroll
@@ -640,6 +745,10 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx(GatedDxArgs a) {
     if (more) put(k0 + KC);
     __syncthreads();
   }
+  if constexpr (RANGED)
+#pragma unroll
+    for (int i = 0; i < RI; i++)
+      if (was_code[i]) change_units(acc[i], was[i], 0);
   constexpr int OP = BN / PE;
 #pragma unroll
   for (int h = 0; h < 2; h++) {
@@ -679,17 +788,26 @@ __global__ __launch_bounds__(512) void k_gated_dx_small(GatedDxArgs a) {
   const int64_t r0 = (int64_t)blockIdx.x * 32, r = min(r0 + l % 32, a.rows - 1);
   const int n0 = blockIdx.y * 32, n = min(n0 + l % 32, a.cols - 1);
   const T *d = static_cast<const T *>(a.d) + r * 2 * a.pad, *gate = static_cast<const T *>(a.gate) + n * a.ld_gate, *up = static_cast<const T *>(a.up) + n * a.ld_up;
-  f32x16 acc = f32x16{};
+  f32x16 acc[1] = {f32x16{}};
+  const int64_t blocks = kRanged<T> ? r0 / 32 * a.range.across : 0;
+  int was = 0;
 #pragma unroll 4
   for (int k0 = wave * KS; k0 < 2 * a.pad; k0 += WAVES * KS) {
     const int at = k0 + half * VK, k = at - (at >= a.pad ? a.pad : 0);
     const Piece dv = *reinterpret_cast<const Piece *>(d + at);
     const Piece wv = piece_of<T, T, SHORT>(raw_piece<T, T, SHORT>(at >= a.pad ? up : gate, k, a.hidden), k, a.hidden);
-    acc = mma(__builtin_bit_cast(V, wv), __builtin_bit_cast(V, dv), acc);
+    if constexpr (kRanged<T>) {                // under no condition: the loads of several steps are then under way together
+      const int code = a.range.unit[blocks + k0 / 32], finer = a.range.finer[(blocks + k0 / 32) * 32 + l % 32];
+      const int now = (code >> 1) - (code & 1 ? finer : 0);
+      change_units(acc, was, now);
+      was = now;
+    }
+    acc[0] = mma(__builtin_bit_cast(V, wv), __builtin_bit_cast(V, dv), acc[0]);
   }
+  if constexpr (kRanged<T>) change_units(acc, was, 0);
 #pragma unroll
   for (int e = 0; e < 4; e++) {
-    const F4 v = {acc[4 * e], acc[4 * e + 1], acc[4 * e + 2], acc[4 * e + 3]};
+    const F4 v = {acc[0][4 * e], acc[0][4 * e + 1], acc[0][4 * e + 2], acc[0][4 * e + 3]};
     *reinterpret_cast<F4 *>(&s_acc[wave][l % 32][8 * e + 4 * half]) = v;
   }
   __syncthreads();
@@ -709,6 +827,7 @@ struct GatedDwArgs {
   float *part;                               // [slices][tiles of d][tiles of x][RI WM][2 WN] fragments
   int64_t rows, ld_x, slice;
   int cols, pad, add, slices, tiles_c, tiles_n;
+  GatedRange range;
 };
 template <class T, int RI, int WM, int WN, bool SHORT>
 __global__ __launch_bounds__(kWave * WM * WN, 2) void k_gated_dw(GatedDwArgs a) {
@@ -740,6 +859,12 @@ __global__ __launch_bounds__(kWave * WM * WN, 2) void k_gated_dw(GatedDwArgs a) 
   Piece x[NX], d[ND];
   const int xc = c0 + tid % CX * PE, dc = n0 + tid % CD * PE;
   const int dc_in = min(dc, 2 * a.pad - PE);
+  // float16: units of the two blocks of rows of a chunk, of this wave's columns of d and of this thread's pieces
+  constexpr bool RANGED = kRanged<T>;
+  static_assert(!RANGED || (KR == 64 && 32 % RD == 0), "a chunk is two blocks of rows");
+  int unit[2][2], next_unit[2][2], piece_unit[2], was[2] = {0, 0};
+  int64_t row_block[2];
+  const int wave_block = min(n0 / 32 + wn * 2, 2 * a.pad / 32 - 2);
   auto fetch = [&](int64_t r0) {             // of the last chunk the last row stands in for those past the slice's end
     const int left = (int)max((int64_t)1, min(r_end - r0, (int64_t)KR));
     const T *xp = static_cast<const T *>(a.x) + min(r0, a.rows - 1) * a.ld_x, *dp = static_cast<const T *>(a.d) + min(r0, a.rows - 1) * 2 * a.pad + dc_in;
@@ -747,6 +872,14 @@ __global__ __launch_bounds__(kWave * WM * WN, 2) void k_gated_dw(GatedDwArgs a) 
     for (int j = 0; j < NX; j++) x[j] = raw_piece<T, T, SHORT>(xp + min(tid / CX + RX * j, left - 1) * a.ld_x, xc, a.cols);
 #pragma unroll
     for (int j = 0; j < ND; j++) d[j] = *reinterpret_cast<const Piece *>(dp + (uint32_t)(min(tid / CD + RD * j, left - 1) * 2 * a.pad));
+    if constexpr (RANGED)
+#pragma unroll
+      for (int q = 0; q < 2; q++) {
+        row_block[q] = min(r0 / 32 + q, (a.rows - 1) / 32) * a.range.across;
+        piece_unit[q] = a.range.unit[row_block[q] + dc_in / 32];
+#pragma unroll
+        for (int n = 0; n < 2; n++) next_unit[q][n] = a.range.unit[row_block[q] + wave_block + n];
+      }
   };
   auto put = [&](int64_t r0) {
     const int left = (int)min(r_end - r0, (int64_t)KR);
@@ -759,6 +892,14 @@ __global__ __launch_bounds__(kWave * WM * WN, 2) void k_gated_dw(GatedDwArgs a) 
 #pragma unroll
     for (int j = 0; j < ND; j++) {
       Piece v = d[j];
+      if constexpr (RANGED)
+        if (piece_unit[RD * j / 32] & 1) {     // to the block's units
+          const int finer = a.range.finer[(row_block[RD * j / 32] + dc_in / 32) * 32 + tid / CD + RD * j % 32];
+          V t = __builtin_bit_cast(V, v);
+#pragma unroll
+          for (int e = 0; e < 8; e++) t[e] = (T)__builtin_amdgcn_ldexpf((float)t[e], -finer);
+          v = __builtin_bit_cast(Piece, t);
+        }
       if (left < KR && tid / CD + RD * j >= left) v = Piece{};
       *reinterpret_cast<Piece *>(s_d + (tid / CD + RD * j) * PD + tid % CD * 16) = v;
     }
@@ -768,10 +909,22 @@ __global__ __launch_bounds__(kWave * WM * WN, 2) void k_gated_dw(GatedDwArgs a) 
   __syncthreads();
   for (int64_t r0 = r_begin; r0 < r_end; r0 += KR) {
     const bool more = r0 + KR < r_end;
+    if constexpr (RANGED)
+#pragma unroll
+      for (int q = 0; q < 4; q++) unit[q / 2][q % 2] = next_unit[q / 2][q % 2] >> 1;
     if (more) fetch(r0 + KR);
 #pragma unroll
     for (int s = 0; s < STEPS; s++) {
       V xs[RI], ds[2];
+      if constexpr (RANGED)
+        if (s % 2 == 0)
+#pragma unroll
+          for (int n = 0; n < 2; n++)
+            if (unit[s / 2][n] != was[n]) {
+#pragma unroll
+              for (int i = 0; i < RI; i++) change_units(reinterpret_cast<f32x16 (&)[1]>(acc[i][n]), was[n], unit[s / 2][n]);
+              was[n] = unit[s / 2][n];
+            }
 #pragma unroll
       for (int n = 0; n < 2; n++) ds[n] = columns_frag<T>(s_d, PD, s, wn * 2 + n);
 #pragma unroll
@@ -787,12 +940,14 @@ __global__ __launch_bounds__(kWave * WM * WN, 2) void k_gated_dw(GatedDwArgs a) 
   for (int i = 0; i < RI; i++) {
     if (i >= blocks) continue;
 #pragma unroll
-    for (int n = 0; n < 2; n++)
+    for (int n = 0; n < 2; n++) {
+      if (kRanged<T> && was[n]) change_units(reinterpret_cast<f32x16 (&)[1]>(acc[i][n]), was[n], 0);
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         const F4 v = {acc[i][n][4 * e], acc[i][n][4 * e + 1], acc[i][n][4 * e + 2], acc[i][n][4 * e + 3]};
         reinterpret_cast<F4 *>(part)[(((wm * RI + i) * 2 * WN + wn * 2 + n) * 4 + e) * 64 + l] = v;
       }
+    }
   }
 }
 
@@ -1051,7 +1206,7 @@ template <class T, class TO> static void gated_run(const GatedArgs &a, Launches 
 // rounding the results alone gives 0.0017).
 static bool grad_of_few(int64_t rows, int hidden) { return rows * hidden <= (rows <= 2 * kFewRows ? kFewResults : rows <= 64 ? 4096 : 0); }
 constexpr int64_t kFullTiles = 64;           // tiles of 128 by 128 from which on they are faster than small ones
-struct GatedPlan { int pad, ri, wm, wn, tiles_c, tiles_n, slices; int64_t part_rows, slice, d_bytes, part_bytes; };
+struct GatedPlan { int pad, ri, wm, wn, tiles_c, tiles_n, slices; int64_t part_rows, slice, d_bytes, range_bytes, part_bytes; };
 static GatedPlan gated_plan(int64_t rows, int cols, int hidden, int type) {
   GatedPlan p{};
   p.pad = (hidden + 31) / 32 * 32;
@@ -1078,12 +1233,19 @@ static GatedPlan gated_plan(int64_t rows, int cols, int hidden, int type) {
   p.slice = (steps + slices - 1) / slices * 64;
   p.slices = (int)(slices >= 8 ? slices : (p.part_rows + p.slice - 1) / p.slice);
   p.d_bytes = p.part_rows * row_bytes;
+  p.range_bytes = type == INK_F16 ? p.part_rows / 32 * (2 * p.pad / 32) * (32 + 4) : 0;
   p.part_bytes = (int64_t)p.slices * tiles * tile_bytes;
   return p;
 }
 
 template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void *work, void *dx, int64_t ld_dx, bool weights, Launches &run) {
   const int64_t rows = a.rows;
+  if (p.range_bytes) {
+    const int64_t blocks = p.range_bytes / 36;
+    a.range.unit = reinterpret_cast<int32_t *>(static_cast<char *>(work) + p.d_bytes);
+    a.range.finer = reinterpret_cast<uint8_t *>(a.range.unit + blocks);
+    a.range.across = 2 * p.pad / 32;
+  }
   const bool brief = is_short<T>(a.cols, a.hidden);
   a.out = work; a.ld_out = 2 * p.pad; a.pad = p.pad;
   for (int64_t r0 = 0; r0 < rows; r0 += p.part_rows) {
@@ -1094,14 +1256,14 @@ template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void 
     const int64_t tiles = (b.rows + 127) / 128;
     if (!stream_run<T, T, true>(b, run)) run(brief ? k_gated_tile<T, T, T, true, true> : k_gated_tile<T, T, T, true, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * ((a.hidden + kTileHidden - 1) / kTileHidden))), dim3(256), b);
     if (dx) {
-      GatedDxArgs q{work, a.gate, a.up, static_cast<T *>(dx) + r0 * ld_dx, b.rows, a.ld_gate, a.ld_up, ld_dx, a.cols, a.hidden, p.pad};
+      GatedDxArgs q{work, a.gate, a.up, static_cast<T *>(dx) + r0 * ld_dx, b.rows, a.ld_gate, a.ld_up, ld_dx, a.cols, a.hidden, p.pad, a.range};
       const int gy = (a.cols + 127) / 128;
       if (tiles * gy < kFullTiles) run(brief ? k_gated_dx_small<T, true> : k_gated_dx_small<T, false>, dim3((unsigned)((b.rows + 31) / 32), (a.cols + 31) / 32), dim3(512), q);
       else run(brief ? k_gated_dx<T, true> : k_gated_dx<T, false>, dim3((unsigned)((tiles + 7) / 8 * 8 * gy)), dim3(256), q);
     }
     if (weights) {
-      GatedDwArgs q{b.x, work, reinterpret_cast<float *>(static_cast<char *>(work) + p.d_bytes), b.rows, a.ld_x, p.slice, a.cols, p.pad, r0 > 0, p.slices,
-                    p.tiles_c, p.tiles_n};
+      GatedDwArgs q{b.x, work, reinterpret_cast<float *>(static_cast<char *>(work) + p.d_bytes + p.range_bytes), b.rows, a.ld_x, p.slice, a.cols, p.pad, r0 > 0, p.slices,
+                    p.tiles_c, p.tiles_n, a.range};
       const auto kernel = p.ri == 4 ? (brief ? k_gated_dw<T, 4, 1, 4, true> : k_gated_dw<T, 4, 1, 4, false>) : (brief ? k_gated_dw<T, 2, 2, 2, true> : k_gated_dw<T, 2, 2, 2, false>);
       run(kernel, dim3((unsigned)(p.slices * p.tiles_c * p.tiles_n)), dim3(256), q);
     }
@@ -1158,7 +1320,7 @@ extern "C" size_t ink_gated_backward_work(int64_t rows, int32_t cols, int32_t hi
   if (!known_type(type) || rows < 1 || gated_check(rows, cols, hidden, INK_ACT_NONE)) return 0;
   if (grad_of_few(rows, hidden)) return (size_t)rows * 2 * hidden * sizeof(float);
   const GatedPlan p = gated_plan(rows, cols, hidden, type);
-  return (size_t)(p.d_bytes + p.part_bytes);
+  return (size_t)(p.d_bytes + p.range_bytes + p.part_bytes);
 }
 
 extern "C" ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int64_t ld_x, const void *w_gate, int64_t ld_gate,
@@ -1195,7 +1357,7 @@ extern "C" ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const vo
   }
   if (weights) {                             // no rows: zeros
     GatedSumArgs s{};
-    s.part = reinterpret_cast<const float *>(static_cast<const char *>(work) + p.d_bytes);
+    s.part = reinterpret_cast<const float *>(static_cast<const char *>(work) + p.d_bytes + p.range_bytes);
     s.d_gate = dw_gate; s.d_up = dw_up; s.ld_gate = ld_dg; s.ld_up = ld_du; s.slices = rows > 0 ? p.slices : 0; s.type = type;
     s.cols = cols; s.hidden = hidden; s.pad = p.pad; s.tiles_c = p.tiles_c; s.tiles_n = p.tiles_n; s.kt = 4; s.nt = 2 * p.wn;
     run(k_gated_sum, dim3((unsigned)((int64_t)p.tiles_c * p.tiles_n * s.kt * s.nt * 16)), dim3(256), s);
