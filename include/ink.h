@@ -364,8 +364,8 @@ ink_status ink_get_stats(ink_ctx *ctx, void *stats_out, size_t bytes);
  *
  * Matrices are row-major, of ink_type elements, row i at i * ld elements.  ld is any number from the
  * row's length up; a matrix that is read may also have ld = 0, one row for all.  Pointers need the alignment of an
- * element only, work memory that of 16 bytes.  rows may be 0 (sums over the rows are then zeros).  Sums and statistics are kept in 32 bits,
- * outputs are rounded once, to nearest even.  NaN and infinities go where the formulas take them.
+ * element only, work memory that of 16 bytes.  rows may be 0 (sums over the rows are then zeros).  Sums and statistics are kept in 32 bits
+ * (but for ink_gated's 16-bit results of 8-bit rows), outputs are rounded once, to nearest even.  NaN and infinities go where the formulas take them.
  * The order of a sum depends on the call's sizes: the same row in a call of other sizes may differ in the last bits.
  *
  * Errors: INK_E_ARG (NULL, misaligned or too little memory, sizes or types out of range, an unknown activation; nothing was
@@ -461,7 +461,10 @@ ink_status ink_rms_norm_backward(const void *dy, int64_t ld_dy, const void *tota
  *   act          ink_act
  * Of 8-bit rows (type INK_E4M3, ink_rms_norm's): row r of x is x_scale[r] times its numbers; the weights lie column by column,
  * [hidden][cols], and column c of Wg is gate_scale[c] times its numbers, of Wu up_scale[c] times; out_type is any of the other three.  The
- * scales are float and not read for other types; x_scale[r] * gate_scale[c] is formed in 32 bits and should be a normal number. */
+ * scales are float and not read for other types; x_scale[r] * gate_scale[c] is formed in 32 bits and should be a normal number.
+ * The sums of 8-bit numbers are those of 32 bits with out_type INK_F32 alone.  For 16-bit results of each eight neighbouring products of a sum (k = 8 i .. 8 i + 7)
+ * what lies below 2^-13 of the largest is dropped: less than 2^-13 of the largest max(|x|, 2^-6) * max(|w|, 2^-6) of the eight, for each of seven.  Typically that
+ * is 1.4e-5 of the result, less than its rounding; where large products cancel it can be more than what is left. */
 ink_status ink_gated(const void *x, int64_t ld_x, const float *x_scale, const void *w_gate, int64_t ld_gate, const void *w_up,
                      int64_t ld_up, const float *gate_scale, const float *up_scale, int64_t rows, int32_t cols, int32_t hidden, int32_t type,
                      int32_t out_type, int32_t act, void *h, int64_t ld_h, void *hip_stream);

@@ -345,7 +345,8 @@ def gated(x, w_gate, w_up, act="silu", x_scale=None, gate_scale=None, up_scale=N
 
     Of 8-bit rows (torch.float8_e4m3fn, rms_norm's) with x_scale [rows] and 8-bit weights with gate_scale and up_scale [hidden] (all
     float32): rows and weights' columns are their numbers times their scales, and out_dtype is float32, bfloat16 (the default) or
-    float16.  8-bit weights are taken as they are where a column's elements are side by side, as in the transpose of a
+    float16.  32-bit results have sums in 32 bits; for 16-bit ones, which take some 0.4 of the time, of every eight neighbouring products what lies below 2^-13 of
+    the largest is dropped: less than the result's rounding but where large products cancel.  8-bit weights are taken as they are where a column's elements are side by side, as in the transpose of a
     contiguous [hidden, cols] tensor; any other layout is copied first."""
     if act not in ACTS:
         raise ValueError("act must be one of %s" % ", ".join(ACTS))
