@@ -489,8 +489,9 @@ ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int6
  *                m_scale times the number of its code, sqrt(v) v_scale times that of its code; zeros everywhere are the moments at the start
  *   step         t, from 1; or step_at, one int64 on the device that holds it (a captured call reads it at every replay; below 1 counts as 1)
  *   seed         of the random numbers that round 8-bit moments and INK_BF16 parameters: up or down, in proportion, so that the expectation of
- *                a parameter, of m and of sqrt(v) is what was to be rounded (that of v is larger by the variance).  The numbers depend on
- *                seed, t, the tensor's id and the element, and on nothing else
+ *                a parameter, of m and of sqrt(v) is what was to be rounded (that of v is larger by the variance); but a root that is not 0 and
+ *                below 2^-9 of its block's scale, 1/229376 of the block's largest, is held at 2^-9 of it, and its element's step is smaller by
+ *                that much.  The numbers depend on seed, t, the tensor's id and the element, and on nothing else
  *   lr and weight_decay 0 .. 1e18;  betas in [0, 1);  eps > 0
  * A gradient that is NaN or infinite makes its element NaN, with 8-bit moments the moments of its block; so does, with 8-bit moments, one
  * whose square is beyond a float (with 32-bit ones its element stays where it is, but for the decay). */

@@ -11,7 +11,8 @@
 // the root, whose logarithm spans half the range.  Sixteen lanes hold such a block; the new scale is their maximum.  A moving average changes by 0.1 % a
 // step, and the numbers of e4m3 lie 6 to 12 % apart: rounded to the nearest it would never move.  So a number between two codes goes to
 // either with the probability of its nearness (the expectation is the number itself), by a random number that is a hash of seed, step, tensor and
-// element.  The root never becomes 0 unless it is: where sqrt(v) in the denominator vanished, the step would be m / eps.  Parameters in bfloat16 are rounded the
+// element.  The root never becomes 0 unless it is: where sqrt(v) in the denominator vanished, the step would be m / eps.  So a root below the smallest code, 2^-9 of
+// the scale, is held there, not rounded by chance: from 1/229376 of the block's largest root down the steps are too small, and never too large.  Parameters in bfloat16 are rounded the
 // same way, for the same reason; a copy in 16 bits, which no step reads again, to the nearest.
 #include <algorithm>
 #include <cmath>

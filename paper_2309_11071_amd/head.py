@@ -445,7 +445,8 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
     is).  moments: adamw_moments', all of one width.  copies: bfloat16 or float16 tensors that get the new float32 parameters (None, or a
     list with None where there is none).  step: the step's number, from 1, or an int64 GPU tensor of one element that holds it.
     grad_scale: a factor of every gradient, a number or a float32 GPU tensor of one element.  seed (64 bits): of the random numbers that round 8-bit
-    moments and bfloat16 parameters up or down in proportion; they depend on seed, step, place in the list and element alone."""
+    moments and bfloat16 parameters up or down in proportion; they depend on seed, step, place in the list and element alone.  Roots of 8-bit second moments below 1/229376
+    of their block's largest are held there."""
     n = len(params)
     if len(grads) != n or len(moments) != n or (copies is not None and len(copies) != n):
         raise ValueError("params, grads, moments and copies must have one entry for each parameter")
