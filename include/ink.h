@@ -483,7 +483,8 @@ ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int6
 /* One step of AdamW over n_tensors tensors, in place: with g = grad * grad_scale (times *grad_scale_at where that is not NULL) and t the step,
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps).
- *   tensors      HOST array, read before the call returns; what its entries point to is DEVICE memory.  No tensor may stand there twice
+ *   tensors      HOST array, read before the call returns; what its entries point to is DEVICE memory.  What the step changes must
+ *                not overlap, nor hold a gradient, step_at or grad_scale_at (INK_E_ARG; INK_E_OOM without host memory to look for that)
  *   param_type   INK_F32 or INK_BF16;  grad_type any;  copy_type INK_BF16 or INK_F16 with INK_F32 parameters, or INK_NO_TYPE
  *   moment_bits  32: m and v are float arrays.  8: m and v are INK_E4M3 arrays, and of each INK_ADAMW_BLOCK neighbouring elements m is
  *                m_scale times the number of its code, sqrt(v) v_scale times that of its code; zeros everywhere are the moments at the start

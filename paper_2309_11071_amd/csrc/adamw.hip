@@ -16,6 +16,8 @@
 // same way, for the same reason; a copy in 16 bits, which no step reads again, to the nearest.
 #include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "head.h"
 
@@ -217,6 +219,38 @@ static const char *adam_tensor_check(const ink_adamw_tensor &t, int param_type, 
   return nullptr;
 }
 
+struct Extent { uintptr_t begin, end; };
+// Whether a step over these tensors changes memory twice, or reads what it changes: workgroups would do so in no order.  What it changes, sorted; the
+// rest is looked up in it.
+static const char *adam_overlap(const ink_adamw_tensor *tensors, int n_tensors, int param_type, int grad_type, int copy_type, bool eight, const int64_t *step_at,
+                                const float *scale_at, Extent *changed) {
+  int n = 0;
+  auto add = [&](const void *p, int64_t bytes) { changed[n++] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}; };
+  for (int i = 0; i < n_tensors; i++) {
+    const ink_adamw_tensor &t = tensors[i];
+    if (!t.n) continue;
+    add(t.param, t.n * type_size(param_type));
+    add(t.m, t.n * (eight ? 1 : 4));
+    add(t.v, t.n * (eight ? 1 : 4));
+    if (copy_type != INK_NO_TYPE) add(t.copy, t.n * type_size(copy_type));
+    if (eight) {
+      add(t.m_scale, (t.n + kAdamBlock - 1) / kAdamBlock * 4);
+      add(t.v_scale, (t.n + kAdamBlock - 1) / kAdamBlock * 4);
+    }
+  }
+  std::sort(changed, changed + n, [](const Extent &a, const Extent &b) { return a.begin < b.begin; });
+  for (int i = 1; i < n; i++)
+    if (changed[i].begin < changed[i - 1].end) return "memory that the step changes stands in the call twice";
+  auto apart = [&](const void *p, int64_t bytes) {               // of disjoint extents in order the last that begins before p + bytes decides
+    const Extent *e = std::lower_bound(changed, changed + n, (uintptr_t)p + (uintptr_t)bytes, [](const Extent &a, uintptr_t at) { return a.begin < at; });
+    return e == changed || e[-1].end <= (uintptr_t)p;
+  };
+  for (int i = 0; i < n_tensors; i++)
+    if (tensors[i].n && !apart(tensors[i].grad, tensors[i].n * type_size(grad_type))) return "a gradient stands in memory that the step changes";
+  if ((step_at && !apart(step_at, 8)) || (scale_at && !apart(scale_at, 4))) return "step_at or grad_scale_at stands in memory that the step changes";
+  return nullptr;
+}
+
 }  // namespace ink
 
 using namespace ink;
@@ -241,6 +275,9 @@ extern "C" ink_status ink_adamw(const ink_adamw_tensor *tensors, int32_t n_tenso
   const bool eight = moment_bits == 8;
   for (int i = 0; i < n_tensors; i++)
     if (const char *why = adam_tensor_check(tensors[i], param_type, grad_type, copy_type, eight)) return fail_call(INK_E_ARG, "%s: tensor %d: %s", who, i, why);
+  const std::unique_ptr<Extent[]> extents(new (std::nothrow) Extent[6 * (size_t)n_tensors + 1]);
+  if (!extents) return fail_call(INK_E_OOM, "%s: no memory to look for tensors that overlap", who);
+  if (const char *why = adam_overlap(tensors, n_tensors, param_type, grad_type, copy_type, eight, step_at, grad_scale_at, extents.get())) return refuse(why);
   AdamArgs a{};
   a.step_at = step_at; a.scale_at = grad_scale_at; a.step = step_at ? 1 : step; a.seed = seed; a.lr = lr;
   a.log_b1 = std::log(beta1); a.log_b2 = std::log(beta2);

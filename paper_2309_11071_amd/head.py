@@ -8,6 +8,7 @@ gradient raises unless it is detached or the call stands under torch.no_grad(). 
 tensor whose rows are contiguous, at any distance from each other; any other layout is copied first.
 Tensors of other devices or types and shapes that do not fit raise.
 """
+import bisect
 import ctypes as C
 import itertools
 import operator
@@ -435,6 +436,15 @@ def _held(ts, name, sizes, dev, dtypes):
     return list(map(_address, ts))
 
 
+def _apart(changed, read):
+    """Raises where extents (begin, end) in `changed` overlap each other, or one in `read` overlaps one of them."""
+    begins, ends = sorted(b for b, _ in changed), sorted(e for _, e in changed)
+    if any(map(operator.gt, ends, begins[1:])):                   # of disjoint extents every one ends before the next begins
+        raise ValueError("tensors that the step changes overlap")
+    if any(bisect.bisect_right(ends, b) != bisect.bisect_left(begins, e) for b, e in read):       # as many end before it as begin before its end
+        raise ValueError("a gradient stands in the memory of a tensor that the step changes")
+
+
 _PARAMS, _COPIES, _CODES, _SCALES = {torch.float32, torch.bfloat16}, {torch.bfloat16, torch.float16}, {E4M3}, {torch.float32}
 
 
@@ -519,6 +529,11 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
     else:
         for kind, entry in zip(zip(*kinds), zip(*columns)):
             groups.setdefault(kind, []).append(entry)
+        extents = [[(x, x + s * w) for x, s, w in zip(column, sizes, widths) if x and s] for column, widths in
+                   ((at, [x.element_size() for x in p]), (c, [2] * n), (held[0], [1 if width == 4 else 4] * n), (held[2], [1 if width == 4 else 4] * n))]
+        extents += [[(x, x + 4 * b) for x, b in zip(held[i], blocks) if b] for i in (1, 3) if held[i]]
+        read = [(x, x + s * y.element_size()) for x, s, y in zip(grad_at, sizes, g) if s]
+        _apart(list(itertools.chain.from_iterable(extents)), read + [(x, x + b) for x, b in ((step_at, 8), (scale_at, 4)) if x])     # (a call finds its own overlaps)
     for (tp, tg, tc), entries in groups.items():
         numbers = list(itertools.chain.from_iterable(entries))
         table = struct.pack("%dq" % len(numbers), *numbers)
