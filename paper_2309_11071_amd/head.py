@@ -4,7 +4,7 @@ projections, log probabilities, each with its gradient, and the step of AdamW th
 Argument marshalling only: every operator runs inside libink.so.  Calls are asynchronous on torch's
 current stream of the tensors' device, like torch's own; results and work memory come from torch's
 allocator.  Nothing is recorded for autograd: the gradients are calls of their own, and a tensor that requires a
-gradient raises unless it is detached or the call stands under torch.no_grad().  A matrix is a 2-D
+gradient raises unless it is detached or the call stands under torch.no_grad(); one with a tangent of forward mode raises unless it is detached.  A matrix is a 2-D
 tensor whose rows are contiguous, at any distance from each other; any other layout is copied first.
 Tensors of other devices or types and shapes that do not fit raise.
 """
@@ -15,6 +15,7 @@ import operator
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import InkError, load_library
 
@@ -55,11 +56,18 @@ def _functions():
     return _fn
 
 
+def _tangent(t, name):
+    """Raises where forward mode would expect a tangent of the result (no_grad() does not concern it)."""
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError("%s has a tangent, and these operators have no forward-mode derivatives: detach it" % name)
+
+
 def _unrecorded(t, name):
-    """Raises where autograd would expect a record of the call; t requires a gradient."""
-    if torch.is_grad_enabled():
+    """Raises where autograd would expect a record of the call."""
+    if t.requires_grad and torch.is_grad_enabled():
         raise ValueError("%s requires a gradient, and these operators record nothing for autograd: detach it or call under torch.no_grad(), "
                          "and use the *_backward calls" % name)
+    _tangent(t, name)
 
 
 def _matrix(t, name, rows=None, cols=None, dtype=None, like=None):
@@ -74,7 +82,7 @@ def _matrix(t, name, rows=None, cols=None, dtype=None, like=None):
         raise ValueError("%s has shape %s, wanted [%s, %s]" % (name, tuple(t.shape), "rows" if rows is None else rows, m if cols is None else cols))
     if like is not None and t.device != like.device:
         raise ValueError("%s is on %s, the rows on %s" % (name, t.device, like.device))
-    if t.requires_grad:
+    if t.requires_grad or forward_ad._current_level >= 0:
         _unrecorded(t, name)
     s0, s1 = t.stride()
     if (s1 != 1 and m > 1) or (s0 < m and s0 != 0 and n > 1):
@@ -91,7 +99,7 @@ def _vector(t, name, n, like, dtypes):
         raise ValueError("%s must be a GPU tensor of shape [%d] on the rows' device" % (name, n))
     if t.dtype not in dtypes:
         raise TypeError("%s has type %s, wanted %s" % (name, t.dtype, " or ".join(str(d) for d in dtypes)))
-    if t.requires_grad:
+    if t.requires_grad or forward_ad._current_level >= 0:
         _unrecorded(t, name)
     return t if n < 2 or t.stride(0) == 1 else t.contiguous()
 
@@ -332,7 +340,7 @@ def _columns_8(w, name, cols, hidden, like):
         raise ValueError("%s must be a GPU tensor of shape [%d, %s] on the rows' device" % (name, cols, "hidden" if hidden is None else hidden))
     if w.dtype is not E4M3:
         raise TypeError("%s has type %s, wanted %s" % (name, w.dtype, E4M3))
-    if w.requires_grad:
+    if w.requires_grad or forward_ad._current_level >= 0:
         _unrecorded(w, name)
     s0, s1 = w.stride()
     if (s0 != 1 and cols > 1) or (s1 < cols and s1 != 0 and w.shape[1] > 1):
@@ -479,8 +487,9 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
         raise ValueError("a parameter that requires a gradient and is no leaf cannot be changed in place")
     if not set(map(_dtype, g)) <= TYPES.keys() or set(map(_device_index, g)) != {dev} or list(map(_shape, g)) != list(map(_shape, p)):
         raise ValueError("a gradient must be a float32, bfloat16 or float16 tensor of its parameter's shape, on its GPU")
-    if any(map(_requires_grad, g)):
-        _unrecorded(g, "a gradient")
+    if any(map(_requires_grad, g)) or forward_ad._current_level >= 0:
+        for x in g:
+            _unrecorded(x, "a gradient")
     if not all(map(_contiguous, g)):
         g = [x.contiguous() for x in g]
     if width == 2:
@@ -500,6 +509,9 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
             c = list(none)
             for i, x in zip(here, _held([copy[i] for i in here], "a copy", [sizes[i] for i in here], dev, _COPIES)):
                 c[i] = x
+    if forward_ad._current_level >= 0:
+        for x in itertools.chain(p, *mom, [copy[i] for i in here]):
+            _tangent(x, "a tensor that the step changes")
     grad_at = list(map(_address, g))
     changed = [*at, *itertools.chain.from_iterable(h for h in held if h), *(x for x in c if x)]
     if not all(sizes):                                                        # tensors without elements have no address of their own
@@ -517,7 +529,7 @@ def adamw(params, grads, moments, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, w
     if isinstance(grad_scale, torch.Tensor):
         if grad_scale.dtype is not torch.float32 or grad_scale.numel() != 1 or grad_scale.get_device() != dev:
             raise ValueError("grad_scale must be a number or a float32 tensor of one element on the parameters' device")
-        if grad_scale.requires_grad:
+        if grad_scale.requires_grad or forward_ad._current_level >= 0:
             _unrecorded(grad_scale, "grad_scale")
         scale_at, grad_scale = grad_scale.data_ptr(), 1.0
     lib = _functions()
