@@ -473,8 +473,9 @@ ink_status ink_gated(const void *x, int64_t ld_x, const float *x_scale, const vo
  * [rows][cols], dw_gate = x^T dg and dw_up = x^T du [cols][hidden], all of `type`; each may be NULL (not wanted).  With 16-bit rows
  * dg and du are rounded to `type` before the products, but for a few rows; those of float16 rows with powers of two beside them, so that they may lie
  * beyond float16's range where the results do not.  The work memory does not grow with the rows beyond 2.1 GB, or
- * 1.1 GB and a matrix of [cols][2 hidden] floats where that has more. */
+ * 1.1 GB and a matrix of [cols][2 hidden] floats where that has more; with dw_gate and dw_up NULL ink_gated_backward_work_dx bytes do, up to 1.1 GB. */
 size_t ink_gated_backward_work(int64_t rows, int32_t cols, int32_t hidden, int32_t type);
+size_t ink_gated_backward_work_dx(int64_t rows, int32_t hidden, int32_t type);
 ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int64_t ld_x, const void *w_gate, int64_t ld_gate,
                               const void *w_up, int64_t ld_up, int64_t rows, int32_t cols, int32_t hidden, int32_t type, int32_t act, void *dx,
                               int64_t ld_dx, void *dw_gate, int64_t ld_dg, void *dw_up, int64_t ld_du, void *work, size_t work_bytes,

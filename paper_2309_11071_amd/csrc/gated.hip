@@ -1326,6 +1326,13 @@ extern "C" size_t ink_gated_backward_work(int64_t rows, int32_t cols, int32_t hi
   return (size_t)(p.d_bytes + p.range_bytes + p.part_bytes);
 }
 
+extern "C" size_t ink_gated_backward_work_dx(int64_t rows, int32_t hidden, int32_t type) {
+  if (!known_type(type) || rows < 1 || gated_check(rows, 1, hidden, INK_ACT_NONE)) return 0;
+  if (grad_of_few(rows, hidden)) return (size_t)rows * 2 * hidden * sizeof(float);
+  const GatedPlan p = gated_plan(rows, 1, hidden, type);         // (parts of the rows do not depend on the columns)
+  return (size_t)(p.d_bytes + p.range_bytes);
+}
+
 extern "C" ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const void *x, int64_t ld_x, const void *w_gate, int64_t ld_gate,
                                          const void *w_up, int64_t ld_up, int64_t rows, int32_t cols, int32_t hidden, int32_t type, int32_t act,
                                          void *dx, int64_t ld_dx, void *dw_gate, int64_t ld_dg, void *dw_up, int64_t ld_du, void *work,
@@ -1341,8 +1348,9 @@ extern "C" ink_status ink_gated_backward(const void *dh, int64_t ld_dh, const vo
   if (dw_gate && !good_matrix(dw_gate, cols, hidden, ld_dg, type, true)) return fail_call(INK_E_ARG, "%s: dw_gate is not aligned to its type or has rows that overlap", who);
   if (dw_up && !good_matrix(dw_up, cols, hidden, ld_du, type, true)) return fail_call(INK_E_ARG, "%s: dw_up is not aligned to its type or has rows that overlap", who);
   const bool weights = dw_gate || dw_up;
-  if (rows > 0 && (dx || weights) && (!work || !aligned_to(work, 16) || work_bytes < ink_gated_backward_work(rows, cols, hidden, type)))
-    return fail_call(INK_E_ARG, "%s: work holds less than ink_gated_backward_work bytes or is not aligned to 16", who);
+  const size_t needed = weights ? ink_gated_backward_work(rows, cols, hidden, type) : ink_gated_backward_work_dx(rows, hidden, type);
+  if (rows > 0 && (dx || weights) && (!work || !aligned_to(work, 16) || work_bytes < needed))
+    return fail_call(INK_E_ARG, "%s: work holds less than ink_gated_backward_work%s bytes or is not aligned to 16", who, weights ? "" : "_dx");
   Launches run(hip_stream);
   GatedArgs a{};
   a.x = x; a.gate = w_gate; a.up = w_up; a.dh = dh;

@@ -49,7 +49,7 @@ def _functions():
             fn.argtypes, fn.restype = args, C.c_int
         for name, args in dict(ink_layer_norm_backward_work=(l, i, i), ink_linear_backward_work=(l, i, i),
                                ink_log_probs_work=(l, l, i, i), ink_rms_norm_backward_work=(l, i, i),
-                               ink_gated_backward_work=(l, i, i, i)).items():
+                               ink_gated_backward_work=(l, i, i, i), ink_gated_backward_work_dx=(l, i, i)).items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, z
         _fn = lib
@@ -403,7 +403,11 @@ def gated_backward(dh, x, w_gate, w_up, act="silu", need_dx=True, need_dweights=
     lib = _functions()
     dx = x.new_empty((rows, cols)) if need_dx else None
     dw_gate, dw_up = (x.new_empty((cols, hidden)), x.new_empty((cols, hidden))) if need_dweights else (None, None)
-    n_work = lib.ink_gated_backward_work(rows, cols, hidden, TYPES[t]) if need_dx or need_dweights else 0
+    n_work = 0
+    if need_dweights:
+        n_work = lib.ink_gated_backward_work(rows, cols, hidden, TYPES[t])
+    elif need_dx:
+        n_work = lib.ink_gated_backward_work_dx(rows, hidden, TYPES[t])
     work = x.new_empty(n_work, dtype=torch.uint8) if n_work else None
     _call(lib.ink_gated_backward, x, dh.data_ptr(), ld_dh, x.data_ptr(), ld, w_gate.data_ptr(), ld_gate, w_up.data_ptr(), ld_up, rows, cols, hidden,
           TYPES[t], ACTS[act], _ptr(dx), cols, _ptr(dw_gate), hidden, _ptr(dw_up), hidden, _ptr(work), n_work)
