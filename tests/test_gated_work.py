@@ -64,5 +64,6 @@ def test_a_calls_memory():
         taken.append(torch.cuda.max_memory_allocated() - before)
         del got
     lib = head._functions()
-    assert taken[0] <= lib.ink_gated_backward_work_dx(rows, hidden, 1) + 2 * rows * cols + 4096
-    assert taken[1] - taken[0] >= lib.ink_gated_backward_work(rows, cols, hidden, 1) - lib.ink_gated_backward_work_dx(rows, hidden, 1)
+    step = 2 << 20                                                # torch's allocator takes memory of this size by whole multiples of 2 MiB: dx and the work memory
+    assert taken[0] <= lib.ink_gated_backward_work_dx(rows, hidden, 1) + 2 * rows * cols + 2 * step
+    assert taken[1] - taken[0] >= lib.ink_gated_backward_work(rows, cols, hidden, 1) - lib.ink_gated_backward_work_dx(rows, hidden, 1) - 2 * step
