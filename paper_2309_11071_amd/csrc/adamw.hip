@@ -28,7 +28,7 @@ static_assert(kAdamBlock == 16 * kAdamEach, "sixteen lanes hold a block");
 
 struct AdamArgs {
   ink_adamw_tensor tensor[kAdamTensors];
-  int32_t first[kAdamTensors + 1];         // of a tensor's workgroups; behind the last tensor the number of all
+  int32_t first[kAdamTensors];             // of a tensor's workgroups; behind the last tensor INT32_MAX
   int32_t tiles;                           // tiles a workgroup takes, one after another
   const int64_t *step_at;                  // the step's number on the device, or NULL
   const float *scale_at;                   // a factor of the gradient on the device, or NULL
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kHeadThreads) void k_adamw(AdamArgs a) {
   int k = 0;
 #pragma unroll
   for (int o = kAdamTensors / 2; o; o >>= 1)
-    if ((int)blockIdx.x >= a.first[k + o]) k += o;             // tensors behind the last have the number of all workgroups there
+    if ((int)blockIdx.x >= a.first[k + o]) k += o;             // no workgroup belongs to places behind the last tensor
   const ink_adamw_tensor t = a.tensor[k];
   const int64_t at = (int64_t)((int)blockIdx.x - a.first[k]) * a.tiles * kAdamTile;
   float by_m = a.by_m, by_v = a.by_v, grad_scale = a.grad_scale;
@@ -300,11 +300,9 @@ extern "C" ink_status ink_adamw(const ink_adamw_tensor *tensors, int32_t n_tenso
     for (a.tiles = 1; a.tiles < 1 << 20 && tiles / a.tiles >= 2 * 16384; a.tiles *= 2) {}
     int64_t groups = 0;
     for (int k = 0; k < kAdamTensors; k++) {
-      a.first[k] = (int32_t)groups;
+      a.first[k] = k < n ? (int32_t)groups : INT32_MAX;
       if (k < n) groups += (a.tensor[k].n + (int64_t)a.tiles * kAdamTile - 1) / ((int64_t)a.tiles * kAdamTile);
     }
-    a.first[kAdamTensors] = (int32_t)groups;
-    for (int k = n; k < kAdamTensors; k++) a.first[k] = INT32_MAX;
     run(kernel, dim3((unsigned)groups), dim3(kHeadThreads), a);
   }
   return run.done(who);

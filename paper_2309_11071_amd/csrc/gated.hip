@@ -1267,7 +1267,9 @@ template <class T> static void gated_grad(GatedArgs a, const GatedPlan &p, void 
     if (weights) {
       GatedDwArgs q{b.x, work, reinterpret_cast<float *>(static_cast<char *>(work) + p.d_bytes + p.range_bytes), b.rows, a.ld_x, p.slice, a.cols, p.pad, r0 > 0, p.slices,
                     p.tiles_c, p.tiles_n, a.range};
-      const auto kernel = p.ri == 4 ? (brief ? k_gated_dw<T, 4, 1, 4, true> : k_gated_dw<T, 4, 1, 4, false>) : (brief ? k_gated_dw<T, 2, 2, 2, true> : k_gated_dw<T, 2, 2, 2, false>);
+      auto kernel = brief ? k_gated_dw<T, 2, 2, 2, true> : k_gated_dw<T, 2, 2, 2, false>;
+      if constexpr (sizeof(T) == 2)
+        if (p.ri == 4) kernel = brief ? k_gated_dw<T, 4, 1, 4, true> : k_gated_dw<T, 4, 1, 4, false>;
       run(kernel, dim3((unsigned)(p.slices * p.tiles_c * p.tiles_n)), dim3(256), q);
     }
   }
