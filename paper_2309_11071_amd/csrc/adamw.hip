@@ -4,8 +4,9 @@
 //   p = p (1 - lr decay) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // Bound by memory: some fifteen operations an element against 28 bytes (32-bit parameters and moments, 16-bit gradient and copy) or 16 (moments in
-// 8 bits), at the rate of a copy (5.09 TB/s): 186M elements in 259 tensors 1025 us (5.20 GB), 27.7M with moments in 8 bits 94 us (448 MB).  One launch takes up to kAdamTensors tensors, whose addresses are its arguments, so that nothing is copied to the device ahead; workgroups take
-// kAdamTile elements or several times that of one tensor and find it by a search over the tensors' first workgroups.  A thread has eight neighbouring elements.
+// 8 bits), at the rate of a copy (5.09 TB/s): 186M elements in 259 tensors 1025 us (5.20 GB), 27.7M with moments in 8 bits 94 us (448 MB).  One launch takes
+// up to kAdamTensors tensors, whose addresses are its arguments, so that nothing is copied to the device ahead; workgroups take kAdamTile elements
+// or several times that of one tensor and find it by a search over the tensors' first workgroups.  A thread has eight neighbouring elements.
 //
 // Moments in 8 bits: of 128 neighbouring elements each has an e4m3 code and all share a scale (their largest magnitude / 448), m as it is, of v
 // the root, whose logarithm spans half the range.  Sixteen lanes hold such a block; the new scale is their maximum.  A moving average changes by 0.1 % a

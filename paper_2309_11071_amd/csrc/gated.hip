@@ -7,9 +7,10 @@
 // As in linear.hip every product is formed transposed, the weights' columns as the instruction's rows, so that a lane ends up with four
 // neighbouring columns of its row, here of g and of u: act(g) u needs nothing of another lane.  Which kernel, forward:
 //
-//   up to 16 rows, 64k results   k_gated_few     a row and 32 columns a workgroup; the weights are what is read: 1 x 256 x 683 bf16 6 us
-//   from 16384 or 32768 rows on  k_gated_stream  the weights in registers, rows in a stream; depths of up to 256 (16 bits), 128 (32 bits) or 512 (8 bits)
-//   else                         k_gated_tile    128 rows by 64 columns, both operands through LDS
+//   up to 16 rows, 64k results   k_gated_few     a row and 32 columns a workgroup; the weights are what is read: 1 x 256 x 683 bf16 6 us; not of 8-bit rows
+//   from 16384 or 32768 rows on  k_gated_stream  the weights in registers, rows in a stream; depths of up to 256 (16 bits), 128 (32 bits) or 512 (8 bits, with
+//                                                16-bit results)
+//   else                         k_gated_tile    128 rows by 64 columns, both operands through LDS; 32-bit results of 8-bit rows at any size
 //
 // What bounds the stream: reading rows and writing h (16 bits, 128 columns), the vector instructions of the activation (8 bits, whose products take a
 // quarter of the time), the matrix unit (32 bits).  Figures at each kernel.
@@ -17,8 +18,8 @@
 // The gradient does not keep g and u: forming them again costs 4 rows cols hidden operations, keeping them 8 bytes an element of h written and
 // read (1M x 128 x 344 bf16: 0.16 ms of the matrix unit against 0.55 ms of memory).  dg and du are left in work memory once, in the rows' type, for the two
 // products that read them: an error of the size of the results' own rounding (233k x 256 x 683 bf16 0.0024 from 64 bits where rounding the results alone
-// gives 0.0017).  float16 rows keep their range besides (GatedRange).  A few rows are kept in 32 bits.  The weights' gradients are sums over all rows: workgroups take slices of the rows and leave a
-// partial matrix each, added up in order (no atomics: the same call gives the same bits).
+// gives 0.0017).  float16 rows keep their range besides (GatedRange).  A few rows are kept in 32 bits.  The weights' gradients are sums over all
+// rows: workgroups take slices of the rows and leave a partial matrix each, added up in order (no atomics: the same call gives the same bits).
 #include <algorithm>
 #include <type_traits>
 
@@ -183,7 +184,8 @@ __device__ __forceinline__ void wave_order() {
 }
 
 // z Phi(z) = max(z, 0) - |z| (1 - Phi(|z|)), with 1 - Phi as normal_cdf has it (half of the polynomial's factors taken in): three instructions fewer
-// than a choice by z's sign, where vector instructions are what the gated pair waits for.  The clamp keeps infinity times 0 away.
+// than a choice by z's sign, which has cost no less time (612.5k x 256 x 1024 of 8 bits 633 us, with the choice 627; 2.45M x 128 x 344 bf16 817 and 815).  The
+// clamp keeps infinity times 0 away.
 __device__ __forceinline__ float gelu(float z) {
   const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118f, fabsf(z), 1.f));
   const float e = __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.4426950408889634f));
@@ -799,7 +801,7 @@ __global__ __launch_bounds__(512) void k_gated_dx_small(GatedDxArgs a) {
     const int at = k0 + half * VK, k = at - (at >= a.pad ? a.pad : 0);
     const Piece dv = *reinterpret_cast<const Piece *>(d + at);
     const Piece wv = piece_of<T, T, SHORT>(raw_piece<T, T, SHORT>(at >= a.pad ? up : gate, k, a.hidden), k, a.hidden);
-    if constexpr (kRanged<T>) {                // under no condition: the loads of several steps are then under way together
+    if constexpr (kRanged<T>) {                // under no condition: sixteen instructions, where the step waits for its loads
       const int code = a.range.unit[blocks + k0 / 32], finer = a.range.finer[(blocks + k0 / 32) * 32 + l % 32];
       const int now = (code >> 1) - (code & 1 ? finer : 0);
       change_units(acc, was, now);
@@ -1124,7 +1126,9 @@ __global__ __launch_bounds__(kHeadThreads) void k_gated_dw_few(GatedFewArgs a) {
 }
 
 // ------------------------------------------------------------------------------------ host side
-constexpr int64_t kFewRows = 16, kFewResults = 64 * 1024;    // as ink_linear: each workgroup asks for its columns of both matrices again for every row
+// As ink_linear: each workgroup asks for its columns of both matrices again for every row, which the caches serve while the weights fit them.  us a call of 16 rows one by one,
+// and of 17 in a tile, bf16: x 256 x 683 8.5 and 8.4 (the binding's time), x 602 x 1605 11.6 and 13.5, x 4096 x 4096 96 and 88, x 16384 x 4096 448 and 329; of one row 8.5, 8.8, 18, 55.
+constexpr int64_t kFewRows = 16, kFewResults = 64 * 1024;
 
 // rows of x or of the weights that hold no whole piece of 16 bytes
 template <class T> static bool is_short(int cols, int hidden) { return std::min(cols, hidden) < 16 / (int)sizeof(T); }
@@ -1148,7 +1152,8 @@ template <class T, class TO, int KS, int WN, int WM, int PER, bool GRAD> static 
 // Four waves a workgroup, one on every SIMD of its CU (workgroups of six leave no room for a second one although its registers are there), or, where the
 // columns fill them about as well, twelve, three on every SIMD: rows of results then leave a workgroup whole, which counts where they are no multiple of
 // whole lines (2.45M x 128 x 341 bf16 722 us with twelve waves, 872 with three workgroups of four; x 344 660 and 765; x 384 654 and 692).  With one or two
-// waves side by side a thread has more of the rows under way and some registers spill, as in linear.hip; their calls wait for the rows.
+// waves side by side a thread has more of the rows under way and registers spill, as in linear.hip: up to 85 (16 bits, 16 steps), 98 (32 bits), 151 (8 bits, 8 steps), all with one wave;
+// their calls wait for the rows.  Of the others the forms of 8-bit rows with 4 steps spill four.
 template <class T, class TO, int KS, int PER, bool GRAD> static void stream_waves(const GatedArgs &a, Launches &run) {
   const int tiles = ((GRAD ? a.pad : a.hidden) + 31) / 32;
   if (tiles == 1) return stream_launch<T, TO, KS, 1, sizeof(T) == 4 ? 2 : 4, PER, GRAD>(a, run);

@@ -1,5 +1,5 @@
-// What the operators of an answer head (norm.hip, linear.hip, probs.hip) share: element types, vectors of them at any
-// address, sums and maxima over groups of lanes, and the checks of their arguments.
+// What the operators of an answer head (norm.hip, linear.hip, probs.hip, rms.hip, gated.hip, adamw.hip) share: element types, vectors
+// of them at any address, sums and maxima over groups of lanes, and the checks of their arguments.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
